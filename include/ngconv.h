@@ -321,6 +321,54 @@ const char *ngc_conv3d_variant(const ngc_conv3d_desc *desc, int op);
  * ngc_conv_kernel says after "rank2:". */
 const char *ngc_conv3d_kernel(const ngc_conv3d_desc *desc, int op);
 
+/* ---- Tokens and a vocabulary ---------------------------------------------------------------------
+ * The nodes at both ends of a model over a vocabulary, next to the Softmax row op: rows from tokens, normalised rows, and the loss of
+ * the last linear layer; derivative nodes as in Sec. 3.  Tensors are dense and element aligned (ids and labels 8 bytes, fp32 vectors
+ * 4 bytes, ws 16 bytes); every [rows, cols] tensor holds fewer than 2^40 elements and has fewer than 2^31 rows.  Sums and statistics
+ * are fp32, results of `dtype` are rounded once, and a result does not depend on timing.  Inputs must be finite. */
+
+/* Embedding lookup: y[t] = scale * table[ids[t]], table: [vocab, width], y: [tokens, width], both of `dtype`.  A token whose id is
+ * outside [0, vocab) has no row (padding): y[t] = +0. */
+int ngc_embedding(int32_t dtype, int64_t tokens, int32_t vocab, int32_t width, float scale, const void *table, const int64_t *ids,
+                  void *y, void *hip_stream);
+
+/* Its gradient: dtable[v] = scale * sum of dy[t] over the tokens with ids[t] = v, in an order that the sizes alone fix; fp32, [vocab, width],
+ * every row overwritten (+0 for rows without tokens).  Ids outside [0, vocab) add nothing.  vocab <= 2^21 (else NGC_BAD_SHAPE).
+ * ws: ngc_embedding_workspace_bytes(tokens, vocab, width) bytes. */
+int ngc_embedding_bwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t width, float scale, const void *dy, const int64_t *ids,
+                      float *dtable, void *ws, size_t ws_bytes, void *hip_stream);
+size_t ngc_embedding_workspace_bytes(int64_t tokens, int32_t vocab, int32_t width);
+
+/* Layer norm over the last axis of a [rows, cols] tensor: mean = sum x / cols, rstd = (sum (x - mean)^2 / cols + eps)^(-1/2),
+ * y = (x - mean) * rstd * gamma + beta.  gamma, beta: fp32 [cols], NULL = 1 and 0.  mean, rstd: fp32 [rows] for the backprop, either
+ * may be NULL.  y may be x.  eps >= 0 and finite (else NGC_BAD_ARG); with eps = 0 a constant row has no result. */
+int ngc_layer_norm(int32_t dtype, int64_t rows, int32_t cols, float eps, const void *x, const float *gamma, const float *beta,
+                   void *y, float *mean, float *rstd, void *hip_stream);
+
+/* Its backprop from x and the statistics of the forward call: with g = dy * gamma and xh = (x - mean) * rstd,
+ *   dx = rstd * (g - mean(g) - xh * mean(g * xh)), dgamma[j] = sum over the rows of dy * xh, dbeta[j] = sum over the rows of dy.
+ * dx: `dtype`, may be dy or x; dgamma, dbeta: fp32 [cols], overwritten, either may be NULL.
+ * ws: ngc_layer_norm_workspace_bytes(dtype, rows, cols) bytes, NULL if neither dgamma nor dbeta is asked for. */
+int ngc_layer_norm_bwd(int32_t dtype, int64_t rows, int32_t cols, const void *x, const float *gamma, const float *mean,
+                       const float *rstd, const void *dy, void *dx, float *dgamma, float *dbeta, void *ws, size_t ws_bytes,
+                       void *hip_stream);
+size_t ngc_layer_norm_workspace_bytes(int32_t dtype, int64_t rows, int32_t cols);
+
+/* Softmax cross entropy of a linear layer: z = x w^T, lse[n] = log sum_v exp z[n][v], loss[n] = lse[n] - z[n][labels[n]].
+ * x: [rows, width], w: [vocab, width], both of `dtype`; loss, lse: fp32 [rows].  A row whose label is outside [0, vocab) does not count:
+ * its loss is +0 (its lse is written).  The logits are formed tile by tile and never kept.
+ * ws: ngc_linear_xent_workspace_bytes(dtype, rows, width, vocab, 0) bytes. */
+int ngc_linear_xent(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, const void *x, const void *w, const int64_t *labels,
+                    float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Its gradients: g[n][v] = (exp(z[n][v] - lse[n]) - [v = labels[n]]) * dloss[n], 0 for the rows that do not count; dx = g w, dw = g^T x, both
+ * of `dtype`, overwritten; either (not both) may be NULL.  lse: of the forward call on the same x and w; dloss: fp32 [rows] (1 / count for a
+ * mean).  The logits are formed again, a piece of the vocabulary at a time.
+ * ws: ngc_linear_xent_workspace_bytes(dtype, rows, width, vocab, 1) bytes. */
+int ngc_linear_xent_bwd(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, const void *x, const void *w, const int64_t *labels,
+                        const float *lse, const float *dloss, void *dx, void *dw, void *ws, size_t ws_bytes, void *hip_stream);
+size_t ngc_linear_xent_workspace_bytes(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, int32_t bwd);
+
 /* Test hook.  The library reads its NGC_* environment switches (kernel-variant overrides for tests and
  * experiments; NGC_DRY_RUN=1 skips every launch after the host-side planning) once per process, at first use,
  * and caches the launch plan of every descriptor it has seen per thread.  This call reads the switches again and

@@ -10,6 +10,9 @@ from .conv_oracle import (  # noqa: F401
     relu_bwd_mask, bias_grad, conv_bwd_data_relu,
 )
 from .softmax_oracle import softmax, softmax_bwd  # noqa: F401
+from .tokens_oracle import (  # noqa: F401
+    embedding, embedding_bwd, layer_norm, layer_norm_bwd, linear_xent, linear_xent_bwd,
+)
 from .conv3d_oracle import (  # noqa: F401
     Attrs3, out_shape3, conv3d_fwd, conv3d_bwd_data, conv3d_bwd_filters, conv3d_fwd_at,
     conv3d_bwd_data_at, conv3d_bwd_filters_at,

@@ -32,7 +32,9 @@ EXPORTS = ("ngc_conv_out_shape", "ngc_conv_workspace_bytes", "ngc_conv_fwd", "ng
            "ngc_conv3d_out_shape", "ngc_conv3d_workspace_bytes", "ngc_conv3d_fwd", "ngc_conv3d_bwd_data",
            "ngc_conv3d_bwd_filters", "ngc_conv3d_filter_convert", "ngc_conv3d_filter_elems", "ngc_conv3d_data_elems",
            "ngc_conv3d_variant", "ngc_conv3d_kernel", "ngc_conv3d_bwd_data_relu", "ngc_conv3d_bwd_data_relu_db", "ngc_conv3d_bias_grad",
-           "ngc_conv_bwd_filters_noalloc", "ngc_static_scratch_bytes", "ngc_reload_switches")
+           "ngc_conv_bwd_filters_noalloc", "ngc_static_scratch_bytes", "ngc_reload_switches",
+           "ngc_embedding", "ngc_embedding_bwd", "ngc_embedding_workspace_bytes", "ngc_layer_norm", "ngc_layer_norm_bwd",
+           "ngc_layer_norm_workspace_bytes", "ngc_linear_xent", "ngc_linear_xent_bwd", "ngc_linear_xent_workspace_bytes")
 
 
 class ngc_conv_desc(ctypes.Structure):
@@ -151,6 +153,20 @@ def _load() -> ctypes.CDLL:
     lib.ngc_conv3d_variant.restype = ctypes.c_char_p
     lib.ngc_conv3d_kernel.argtypes = [D3, ctypes.c_int]
     lib.ngc_conv3d_kernel.restype = ctypes.c_char_p
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    lib.ngc_embedding.argtypes = [i32, i64, i32, i32, f32, vp, vp, vp, vp]
+    lib.ngc_embedding_bwd.argtypes = [i32, i64, i32, i32, f32, vp, vp, vp, vp, sz, vp]
+    lib.ngc_embedding_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.ngc_layer_norm.argtypes = [i32, i64, i32, f32, vp, vp, vp, vp, vp, vp, vp]
+    lib.ngc_layer_norm_bwd.argtypes = [i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ngc_layer_norm_workspace_bytes.argtypes = [i32, i64, i32]
+    lib.ngc_linear_xent.argtypes = [i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ngc_linear_xent_bwd.argtypes = [i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ngc_linear_xent_workspace_bytes.argtypes = [i32, i64, i32, i32, i32]
+    for f in (lib.ngc_embedding, lib.ngc_embedding_bwd, lib.ngc_layer_norm, lib.ngc_layer_norm_bwd, lib.ngc_linear_xent, lib.ngc_linear_xent_bwd):
+        f.restype = ctypes.c_int
+    for f in (lib.ngc_embedding_workspace_bytes, lib.ngc_layer_norm_workspace_bytes, lib.ngc_linear_xent_workspace_bytes):
+        f.restype = sz
     return lib
 
 
@@ -307,6 +323,50 @@ def ngc_layout_convert(dtype, n, c, h, w, src, src_layout, dst, dst_layout, stre
 def ngc_filter_convert(desc, w_kcrs, w_blocked, dst_layout, stream=None, check: bool = True) -> int:
     return _check(_lib.ngc_filter_convert(ctypes.byref(desc), _ptr(w_kcrs), _ptr(w_blocked), dst_layout,
                                           _stream(stream)), "ngc_filter_convert", check)
+
+
+# ---- Tokens and a vocabulary: embedding, layer norm, softmax cross entropy of a linear layer
+
+def ngc_embedding(dtype, tokens, vocab, width, scale, table, ids, y, stream=None, check: bool = True) -> int:
+    st = _call.ngc_embedding(dtype, tokens, vocab, width, scale, table, ids, y, stream)
+    return _fail(st, "ngc_embedding") if st and check else st
+
+
+def ngc_embedding_workspace_bytes(tokens, vocab, width) -> int:
+    return int(_lib.ngc_embedding_workspace_bytes(tokens, vocab, width))
+
+
+def ngc_embedding_bwd(dtype, tokens, vocab, width, scale, dy, ids, dtable, ws=None, stream=None, check: bool = True) -> int:
+    st = _call.ngc_embedding_bwd(dtype, tokens, vocab, width, scale, dy, ids, dtable, ws, stream)
+    return _fail(st, "ngc_embedding_bwd") if st and check else st
+
+
+def ngc_layer_norm(dtype, rows, cols, eps, x, gamma, beta, y, mean=None, rstd=None, stream=None, check: bool = True) -> int:
+    st = _call.ngc_layer_norm(dtype, rows, cols, eps, x, gamma, beta, y, mean, rstd, stream)
+    return _fail(st, "ngc_layer_norm") if st and check else st
+
+
+def ngc_layer_norm_workspace_bytes(dtype, rows, cols) -> int:
+    return int(_lib.ngc_layer_norm_workspace_bytes(dtype, rows, cols))
+
+
+def ngc_layer_norm_bwd(dtype, rows, cols, x, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, ws=None, stream=None, check: bool = True) -> int:
+    st = _call.ngc_layer_norm_bwd(dtype, rows, cols, x, gamma, mean, rstd, dy, dx, dgamma, dbeta, ws, stream)
+    return _fail(st, "ngc_layer_norm_bwd") if st and check else st
+
+
+def ngc_linear_xent_workspace_bytes(dtype, rows, width, vocab, bwd=False) -> int:
+    return int(_lib.ngc_linear_xent_workspace_bytes(dtype, rows, width, vocab, 1 if bwd else 0))
+
+
+def ngc_linear_xent(dtype, rows, width, vocab, x, w, labels, loss, lse, ws=None, stream=None, check: bool = True) -> int:
+    st = _call.ngc_linear_xent(dtype, rows, width, vocab, x, w, labels, loss, lse, ws, stream)
+    return _fail(st, "ngc_linear_xent") if st and check else st
+
+
+def ngc_linear_xent_bwd(dtype, rows, width, vocab, x, w, labels, lse, dloss, dx, dw, ws=None, stream=None, check: bool = True) -> int:
+    st = _call.ngc_linear_xent_bwd(dtype, rows, width, vocab, x, w, labels, lse, dloss, dx, dw, ws, stream)
+    return _fail(st, "ngc_linear_xent_bwd") if st and check else st
 
 
 # ---- Convolution over three spatial axes

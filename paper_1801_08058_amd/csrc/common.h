@@ -785,6 +785,21 @@ struct SoftmaxPlan {
 SoftmaxPlan softmax_plan(int dtype, int cols, bool bwd);
 hipError_t launch_softmax(int dtype, bool bwd, const void *a, const void *b, void *out, uint32_t rows, int cols, bool aligned,
                           hipStream_t st);
+hipError_t launch_embedding(int dtype, int64_t tokens, int vocab, int width, float scale, const void *table, const int64_t *ids, void *y,
+                            hipStream_t st);
+size_t embedding_bwd_workspace(int64_t tokens, int vocab, int width);
+hipError_t launch_embedding_bwd(int dtype, int64_t tokens, int vocab, int width, float scale, const void *dy, const int64_t *ids, float *dtable,
+                                void *ws, hipStream_t st);
+hipError_t launch_layer_norm(int dtype, int rows, int cols, float eps, const void *x, const float *gamma, const float *beta, void *y, float *mean,
+                             float *rstd, hipStream_t st);
+size_t layer_norm_bwd_workspace(int dtype, int rows, int cols);
+hipError_t launch_layer_norm_bwd(int dtype, int rows, int cols, const void *x, const float *gamma, const float *mean, const float *rstd,
+                                 const void *dy, void *dx, float *dgamma, float *dbeta, void *ws, hipStream_t st);
+size_t linear_xent_workspace(int dtype, int64_t rows, int width, int vocab, bool bwd);
+hipError_t launch_linear_xent(int dtype, int rows, int width, int vocab, const void *x, const void *w, const int64_t *labels, float *loss, float *lse,
+                              void *ws, hipStream_t st);
+hipError_t launch_linear_xent_bwd(int dtype, int rows, int width, int vocab, const void *x, const void *w, const int64_t *labels, const float *lse,
+                                  const float *dloss, void *dx, void *dw, void *ws, hipStream_t st);
 hipError_t launch_bias_grad(const ngc_conv_desc &d, int P, int Q, const void *dy, float *db, float *partial, int nparts,
                             hipStream_t st);
 int bias_grad_parts(const ngc_conv_desc &d, int P, int Q);

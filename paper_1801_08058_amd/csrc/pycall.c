@@ -131,15 +131,23 @@ ENTRY(ngc_conv3d_bwd_data_relu_db, 1, 7, 1, (&x.d3, x.p[0], x.p[1], x.p[2], x.p[
 ENTRY(ngc_conv3d_bias_grad, 1, 4, 1, (&x.d3, x.p[0], x.p[1], x.p[2], x.ws_bytes, x.p[3]))
 ENTRY(ngc_conv3d_bwd_filters, 1, 5, 1, (&x.d3, x.p[0], x.p[1], x.p[2], x.p[3], x.ws_bytes, x.p[4]))
 
-/* entry points whose leading arguments are integers: KINDS holds 'i' (integer), 'p' (pointer) or 's' (stream) per argument */
-static int parse_kinds(PyObject *const *a, Py_ssize_t n, const char *kinds, long long *i, void **p)
+/* entry points without a descriptor: KINDS holds 'i' (integer), 'f' (float), 'p' (pointer), 'w' (workspace: a pointer whose bytes count)
+ * or 's' (stream) per argument */
+static int parse_kinds(PyObject *const *a, Py_ssize_t n, const char *kinds, long long *i, double *f, size_t *ws_bytes, void **p)
 {
     if (n != (Py_ssize_t)strlen(kinds)) {
         PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
         return -1;
     }
-    for (Py_ssize_t k = 0; k < n; ++k)
+    for (Py_ssize_t k = 0; k < n; ++k) {
+        if (kinds[k] == 'f') {
+            *f = PyFloat_AsDouble(a[k]);
+            if (*f++ == -1.0 && PyErr_Occurred()) return -1;
+            continue;
+        }
+        if (kinds[k] == 'w' && as_bytes(a[k], ws_bytes)) return -1;
         if (kinds[k] == 'i' ? as_int(a[k], i++) : kinds[k] == 's' ? as_stream(a[k], p++) : as_ptr(a[k], p++)) return -1;
+    }
     return 0;
 }
 
@@ -148,9 +156,11 @@ static int parse_kinds(PyObject *const *a, Py_ssize_t n, const char *kinds, long
     static PyObject *w_##NAME(PyObject *self, PyObject *const *a, Py_ssize_t n)             \
     {                                                                                       \
         long long i[8];                                                                     \
-        void *p[8];                                                                         \
-        (void)self;                                                                         \
-        if (parse_kinds(a, n, KINDS, i, p)) return NULL;                                    \
+        double f[2];                                                                        \
+        size_t wb = 0;                                                                      \
+        void *p[12];                                                                        \
+        (void)self; (void)f;                                                                \
+        if (parse_kinds(a, n, KINDS, i, f, &wb, p)) return NULL;                            \
         int rc;                                                                             \
         Py_BEGIN_ALLOW_THREADS                                                              \
         rc = f_##NAME CALL;                                                                 \
@@ -162,6 +172,16 @@ ENTRY_KINDS(ngc_softmax, "iiipps", ((int32_t)i[0], i[1], (int32_t)i[2], p[0], p[
 ENTRY_KINDS(ngc_softmax_bwd, "iiippps", ((int32_t)i[0], i[1], (int32_t)i[2], p[0], p[1], p[2], p[3]))
 ENTRY_KINDS(ngc_layout_convert, "iiiiipipis",
             ((int32_t)i[0], (int32_t)i[1], (int32_t)i[2], (int32_t)i[3], (int32_t)i[4], p[0], (int32_t)i[5], p[1], (int32_t)i[6], p[2]))
+/* sizes past 32 bits are refused by the callee, not cut off here */
+#define I32(k) ((int32_t)(i[k] < INT32_MIN || i[k] > INT32_MAX ? -1 : i[k]))
+ENTRY_KINDS(ngc_embedding, "iiiifppps", (I32(0), i[1], I32(2), I32(3), (float)f[0], p[0], p[1], p[2], p[3]))
+ENTRY_KINDS(ngc_embedding_bwd, "iiiifpppws", (I32(0), i[1], I32(2), I32(3), (float)f[0], p[0], p[1], p[2], p[3], wb, p[4]))
+ENTRY_KINDS(ngc_layer_norm, "iiifpppppps", (I32(0), i[1], I32(2), (float)f[0], p[0], p[1], p[2], p[3], p[4], p[5], p[6]))
+ENTRY_KINDS(ngc_layer_norm_bwd, "iiippppppppws",
+            (I32(0), i[1], I32(2), p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], wb, p[9]))
+ENTRY_KINDS(ngc_linear_xent, "iiiipppppws", (I32(0), i[1], I32(2), I32(3), p[0], p[1], p[2], p[3], p[4], p[5], wb, p[6]))
+ENTRY_KINDS(ngc_linear_xent_bwd, "iiiipppppppws",
+            (I32(0), i[1], I32(2), I32(3), p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], wb, p[8]))
 
 static const struct {
     const char *name;
@@ -172,6 +192,7 @@ static const struct {
     SLOT(ngc_conv_bwd_filters), SLOT(ngc_conv_bwd_filters_noalloc), SLOT(ngc_conv_bwd_data_filters), SLOT(ngc_conv_bwd_data_filters_relu),
     SLOT(ngc_conv3d_fwd), SLOT(ngc_conv3d_bwd_data), SLOT(ngc_conv3d_bwd_data_relu), SLOT(ngc_conv3d_bwd_data_relu_db),
     SLOT(ngc_conv3d_bias_grad), SLOT(ngc_conv3d_bwd_filters), SLOT(ngc_softmax), SLOT(ngc_softmax_bwd), SLOT(ngc_layout_convert),
+    SLOT(ngc_embedding), SLOT(ngc_embedding_bwd), SLOT(ngc_layer_norm), SLOT(ngc_layer_norm_bwd), SLOT(ngc_linear_xent), SLOT(ngc_linear_xent_bwd),
 #undef SLOT
 };
 
@@ -223,6 +244,7 @@ static PyMethodDef methods[] = {
     METHOD(ngc_conv_bwd_filters), METHOD(ngc_conv_bwd_filters_noalloc), METHOD(ngc_conv_bwd_data_filters), METHOD(ngc_conv_bwd_data_filters_relu),
     METHOD(ngc_conv3d_fwd), METHOD(ngc_conv3d_bwd_data), METHOD(ngc_conv3d_bwd_data_relu), METHOD(ngc_conv3d_bwd_data_relu_db),
     METHOD(ngc_conv3d_bias_grad), METHOD(ngc_conv3d_bwd_filters), METHOD(ngc_softmax), METHOD(ngc_softmax_bwd), METHOD(ngc_layout_convert),
+    METHOD(ngc_embedding), METHOD(ngc_embedding_bwd), METHOD(ngc_layer_norm), METHOD(ngc_layer_norm_bwd), METHOD(ngc_linear_xent), METHOD(ngc_linear_xent_bwd),
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", NULL, -1, methods, NULL, NULL, NULL, NULL};
