@@ -1,0 +1,244 @@
+// Matrix products of bf16 operands with fp32 sums for the linear cross entropy (gfx950), with the operands as they lie in memory:
+//
+//   c[m][n] = sum_k A(m, k) B(n, k)      A stored [M][K] or (AT) [K][M], B stored [N][K] or (BT) [K][N]
+//
+// A workgroup of WM x WN waves forms a BM x BN tile; a wave BM/WM x BN/WN of it from v_mfma_f32_16x16x32_bf16, whose first operand is B:
+// an accumulator then holds four neighbouring n of one m.  The reduction runs in stages of 32 through a ring of NS stages in LDS, filled by
+// direct global->LDS loads (16 bytes a lane, the scalar base moves along k).  While the products of a stage run, its successor goes from LDS
+// to registers and the stage NS ahead is asked for: one barrier and one counted wait per stage.
+//
+// LDS of a stage, in units of 16 bytes so that 64 lanes fill 1 KB in lane order:
+//   [R][K] operands   rows of 64 bytes; chunk c of row r sits at c ^ (r / 4 % 4): 16 rows at one chunk touch every bank once
+//   [K][R] operands   blocks of 8 k x 64 columns, rows of 128 bytes; the 32-byte piece b of a row k sits at b ^ (k / 2 % 2) ^ 2 (k / 8 % 2), and
+//                     ds_read_b64_tr_b16 turns 4 k x 16 columns into four k of one column per lane: two lane groups touch every bank once
+// Rows and k past the ends are read as zeros: lanes whose offset is past the range of the buffer descriptor.
+#pragma once
+#include "common.h"
+
+#include <type_traits>
+
+namespace ngc {
+
+typedef __bf16 mm_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float mm_f32x4 __attribute__((ext_vector_type(4)));
+typedef short mm_s16x4 __attribute__((ext_vector_type(4)));
+typedef short mm_s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void mm_lds_void;
+typedef __attribute__((address_space(3))) mm_s16x4 mm_lds_s16x4;
+
+constexpr unsigned MM_OOB = 0x80000000u;
+
+struct MmParams {
+    const uint16_t *a, *b;
+    int64_t lda, ldb;            // elements between rows as stored, multiples of 8; a, b on the 16-byte grid
+    // K: rows of a [K][.] operand past it are not read; a [.][K] operand is read in whole groups of 8, and what lies behind K there has to be
+    // zero.  M / N of an operand that is stored [K][.]: a multiple of 8.
+    int M, N, K;
+    int mt, nt, splits, kper;    // tiles; parts of the reduction and their length (a multiple of 32)
+};
+
+template <int R, bool T, int NW>
+struct MmOperand {
+    static constexpr int LOADS = R / 16 / NW;                            // 1 KB loads per wave and stage
+    static_assert(R % 64 == 0 && LOADS >= 1, "tile");
+    uint64_t base;                                                       // of the tile's first row / column, first k of the part
+    uint64_t step;                                                       // bytes per stage
+    unsigned voff[LOADS];
+
+    // column / row and k within the tile and stage of what a lane loads
+    __device__ static __forceinline__ int rin(int i, int wave)
+    {
+        const int lane = threadIdx.x & 63, q = i * NW + wave;
+        if constexpr (!T) return q * 16 + (lane >> 2);
+        const int kg = q / (R / 64), nb = q % (R / 64), row = lane >> 3, c = lane & 7;
+        return nb * 64 + (((c >> 1) ^ ((row >> 1) & 1) ^ (2 * (kg & 1))) << 4) + (c & 1) * 8;
+    }
+    __device__ static __forceinline__ int kin(int i, int wave)
+    {
+        const int lane = threadIdx.x & 63, q = i * NW + wave;
+        return T ? 8 * (q / (R / 64)) + (lane >> 3) : 8 * ((lane & 3) ^ ((rin(i, wave) >> 2) & 3));
+    }
+    __device__ __forceinline__ void init(const uint16_t *p, int64_t ld, int r0, int extent, int k0, int wave)
+    {
+        base = reinterpret_cast<uint64_t>(p) + 2 * (T ? (int64_t)k0 * ld + r0 : (int64_t)r0 * ld + k0);
+        step = 2 * (T ? 32 * ld : 32);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = rin(i, wave), k = kin(i, wave);
+            voff[i] = r0 + r < extent ? 2u * (unsigned)(T ? k * (int)ld + r : r * (int)ld + k) : MM_OOB;
+        }
+    }
+    // Load i of the stage.  kleft: k that are left from this stage on; FULL: at least 32.  The load goes straight to LDS and has no result
+    // register.  It is written out because the compiler waits for every such load that it knows of in front of a transposing LDS read, whatever
+    // part of the ring that reads; the waits that are needed are those of mm_tile.
+    template <bool FULL>
+    __device__ __forceinline__ void load(int i, unsigned lds, int wave, int kleft) const
+    {
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        const u32x4 rs = {(unsigned)base, (unsigned)(base >> 32) & 0xFFFFu, 0x7fffffffu, 0x00020000u};
+        const unsigned v = FULL || kin(i, wave) < kleft ? voff[i] : MM_OOB;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + (unsigned)(i * NW + wave) * 1024u), "v"(v), "s"(rs));
+    }
+    __device__ __forceinline__ void next() { base += step; }
+};
+
+// this lane's part of the operand of 16 rows / columns: k 8 (lane / 16) .. + 7
+template <int R, bool T>
+struct MmFragments {
+    unsigned at[T ? 4 : 1];
+    __device__ __forceinline__ void init(int r0, int lane)               // r0: first row / column of the wave, a multiple of 16
+    {
+        const int g = lane >> 4, l = lane & 15;
+        if constexpr (T) {
+            const int i = l >> 2, key = ((i >> 1) & 1) ^ (2 * (g & 1));
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                at[b] = (unsigned)(g * (R / 64) * 1024 + (r0 >> 6) * 1024 + i * 128 + (((((r0 >> 4) + b) & 3) ^ key) << 5) + (l & 3) * 8 +
+                                   ((((r0 >> 4) & 3) + b) >> 2) * 1024);
+        } else {
+            at[0] = (unsigned)((r0 + l) * 64 + ((g ^ (l >> 2)) << 4));
+        }
+    }
+    __device__ __forceinline__ mm_bf16x8 read(const unsigned char *lds, int f) const
+    {
+        if constexpr (T) {
+            const unsigned char *p = lds + at[f & 3] + (f >> 2) * 1024;
+            const mm_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mm_lds_s16x4 *)p);
+            const mm_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mm_lds_s16x4 *)(p + 512));
+            return __builtin_bit_cast(mm_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            return *reinterpret_cast<const mm_bf16x8 *>(lds + at[0] + f * 1024);
+        }
+    }
+};
+
+constexpr int MM_STAGES = 4;
+template <int BM, int BN> constexpr int mm_lds_bytes() { return MM_STAGES * (BM + BN) * 64; }
+
+// acc[j] += b a[j]^T for the FM fragments of a row.  Written out so that the accumulators stay where they are: 256 of them fill the
+// accumulation registers, and the compiler moves them about instead of updating them in place.  The leading wait is the one a matrix
+// instruction needs behind a vector instruction that wrote an operand; mm_settle is the one in front of the first read of a result.
+template <int FM>
+__device__ __forceinline__ void mm_row(mm_f32x4 (&acc)[FM], const mm_bf16x8 &b, const mm_bf16x8 (&a)[FM])
+{
+#define NGC_MFMA "v_mfma_f32_16x16x32_bf16 "
+    if constexpr (FM == 8)
+        asm volatile("s_nop 1\n\t" NGC_MFMA "%0, %8, %9, %0\n\t" NGC_MFMA "%1, %8, %10, %1\n\t" NGC_MFMA "%2, %8, %11, %2\n\t" NGC_MFMA "%3, %8, %12, %3\n\t"
+                     NGC_MFMA "%4, %8, %13, %4\n\t" NGC_MFMA "%5, %8, %14, %5\n\t" NGC_MFMA "%6, %8, %15, %6\n\t" NGC_MFMA "%7, %8, %16, %7"
+                     : "+a"(acc[0]), "+a"(acc[1]), "+a"(acc[2]), "+a"(acc[3]), "+a"(acc[4]), "+a"(acc[5]), "+a"(acc[6]), "+a"(acc[7])
+                     : "v"(b), "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]));
+    else if constexpr (FM == 4)
+        asm volatile("s_nop 1\n\t" NGC_MFMA "%0, %4, %5, %0\n\t" NGC_MFMA "%1, %4, %6, %1\n\t" NGC_MFMA "%2, %4, %7, %2\n\t" NGC_MFMA "%3, %4, %8, %3"
+                     : "+a"(acc[0]), "+a"(acc[1]), "+a"(acc[2]), "+a"(acc[3])
+                     : "v"(b), "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]));
+    else
+        asm volatile("s_nop 1\n\t" NGC_MFMA "%0, %2, %3, %0\n\t" NGC_MFMA "%1, %2, %4, %1" : "+a"(acc[0]), "+a"(acc[1]) : "v"(b), "v"(a[0]), "v"(a[1]));
+    static_assert(FM == 8 || FM == 4 || FM == 2, "fragments of a row");
+#undef NGC_MFMA
+}
+template <int FN, int FM>
+__device__ __forceinline__ void mm_settle(mm_f32x4 (&acc)[FN][FM])
+{
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) asm volatile("" : "+a"(acc[i][j]));         // no read of it moves in front of the wait
+}
+
+// Tile of a workgroup: ids go round-robin to the 8 XCDs (one L2 each); each XCD gets a run of tiles, in groups of 8 rows of tiles, so that
+// the tiles that run together share operands in its L2.
+__device__ __forceinline__ void mm_tile_of(int id, int total, int mt, int nt, int &tm, int &tn)
+{
+    const int xcd = id & 7, each = total >> 3, more = total & 7;
+    const int lin = xcd * each + (xcd < more ? xcd : more) + (id >> 3);
+    const int group = lin / (8 * nt), first = group * 8, rows = mt - first < 8 ? mt - first : 8, in = lin - group * 8 * nt;
+    tm = first + in % rows;
+    tn = in / rows;
+}
+
+// acc[fn][fm]: n = 16 fn + 4 (lane / 16) + element, m = 16 fm + lane % 16 of the wave's part
+template <int BM, int BN, int WM, int WN, bool AT, bool BT>
+__device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, int m0, int n0, int k0, int k1, mm_f32x4 (&acc)[BN / WN / 16][BM / WM / 16])
+{
+    constexpr int NW = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, STAGE = (BM + BN) * 64, NS = MM_STAGES;
+    constexpr int LPS = MmOperand<BM, AT, NW>::LOADS + MmOperand<BN, BT, NW>::LOADS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    MmOperand<BM, AT, NW> la;
+    MmOperand<BN, BT, NW> lb;
+    la.init(p.a, p.lda, m0, p.M, k0, wave);
+    lb.init(p.b, p.ldb, n0, p.N, k0, wave);
+    MmFragments<BM, AT> ra;
+    MmFragments<BN, BT> rb;
+    ra.init((wave % WM) * (BM / WM), lane);
+    rb.init((wave / WM) * (BN / WN), lane);
+    const int steps = (k1 - k0 + 31) / 32, full = (k1 - k0) / 32;
+    const unsigned ring = (unsigned)(uintptr_t)(mm_lds_void *)smem;          // LDS address
+    constexpr int LA = MmOperand<BM, AT, NW>::LOADS, LB = MmOperand<BN, BT, NW>::LOADS;
+    mm_bf16x8 fa[2][FM], fb[2][FN];
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) acc[i][j] = mm_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < NS && s < steps; ++s) {
+#pragma unroll
+        for (int i = 0; i < LA; ++i) la.template load<false>(i, ring + s * STAGE, wave, k1 - k0 - 32 * s);
+#pragma unroll
+        for (int i = 0; i < LB; ++i) lb.template load<false>(i, ring + s * STAGE + BM * 64, wave, k1 - k0 - 32 * s);
+        la.next();
+        lb.next();
+    }
+    // the first stage has landed when at most the loads of the three others are under way
+    if (steps >= NS) wait_vmcnt63(LPS * (NS - 1));
+    else wait_vmcnt63(0);
+    wg_barrier_nofence();
+#pragma unroll
+    for (int f = 0; f < FM; ++f) fa[0][f] = ra.read(smem, f);
+#pragma unroll
+    for (int f = 0; f < FN; ++f) fb[0][f] = rb.read(smem + BM * 64, f);
+    // Stage t: its products, between them the LDS reads of stage t + 1 and the loads of stage t + NS.  FULL: both exist, the latter whole.
+    auto stage = [&](auto whole, int t, int u) {
+        constexpr bool FULL = decltype(whole)::value;
+        // stage t + 1 has landed, and this wave has stage t in registers: after the barrier its place in the ring is free
+        if (FULL || t + NS - 1 < steps) wait_vmcnt63(LPS * (NS - 2));
+        else wait_vmcnt63(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);                                  // lgkmcnt(0)
+        wg_barrier_nofence();
+        const unsigned char *next = smem + ((t + 1) % NS) * STAGE;            // past the end: what is left in the ring, not used
+        const unsigned to = ring + (t % NS) * STAGE;
+        const int kleft = k1 - k0 - 32 * (t + NS);
+        const bool more = FULL || t + NS < steps;
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+#pragma unroll
+            for (int f = i * (FM + FN) / FN; f < (i + 1) * (FM + FN) / FN; ++f) {
+                if (f < FM) fa[u ^ 1][f] = ra.read(next, f);
+                else fb[u ^ 1][f - FM] = rb.read(next + BM * 64, f - FM);
+            }
+            if (more)
+#pragma unroll
+                for (int f = i * LPS / FN; f < (i + 1) * LPS / FN; ++f) {
+                    if (f < LA) la.template load<FULL>(f, to, wave, kleft);
+                    else lb.template load<FULL>(f - LA, to + BM * 64, wave, kleft);
+                }
+            mm_row(acc[i], fb[u][i], fa[u]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        la.next();
+        lb.next();
+    };
+    int s = 0;
+    for (; s + NS + 1 < full; s += 2) {
+        stage(std::true_type(), s, 0);
+        stage(std::true_type(), s + 1, 1);
+    }
+    for (; s < steps; s += 2) {
+        stage(std::false_type(), s, 0);
+        if (s + 1 < steps) stage(std::false_type(), s + 1, 1);
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    mm_settle(acc);
+    wg_barrier_nofence();                                                // the ring is free for the caller
+}
+
+}  // namespace ngc
