@@ -157,10 +157,12 @@ __global__ __launch_bounds__(GL <= 64 ? 256 : GL) void layer_norm_bwd_reg(const 
         if (row < rows) nmu = mean[row], nrs = rstd[row];
     };
     const float inv = 1.0f / (float)cols;
-    load((int64_t)blockIdx.x * RPW + group);
+    constexpr bool AHEAD = V * E <= 16;                  // the next row is loaded under this one's sums (else the registers do not hold it)
+    if (AHEAD) load((int64_t)blockIdx.x * RPW + group);
     int slot = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * RPW; r0 < rows; r0 += (int64_t)gridDim.x * RPW, slot ^= 1) {
         const int64_t row = r0 + group;
+        if (!AHEAD) load(row);
         const float mu = nmu, rs = nrs;
         uint4 cx[V], cy[V];
         float2 s = make_float2(0.f, 0.f);
@@ -180,9 +182,13 @@ __global__ __launch_bounds__(GL <= 64 ? 256 : GL) void layer_norm_bwd_reg(const 
                 db[j][e] += d;
             }
         }
+        if (!AHEAD) {
+            keep_packed(cx);
+            keep_packed(cy);
+        }
         if constexpr (GL <= 64) s = make_float2(group_sum<GL>(s.x), group_sum<GL>(s.y));
         else s = block_sum2<NW>(s, sm[slot]);
-        load(row + (int64_t)gridDim.x * RPW);            // behind the wait for this row
+        if (AHEAD) load(row + (int64_t)gridDim.x * RPW);                 // behind the wait for this row
         if (row >= rows) continue;
         const float ma = s.x * inv, mb = s.y * inv;
 #pragma unroll
@@ -426,10 +432,13 @@ static NormPlan norm_plan(int dtype, int rows, int cols, bool bwd)
 {
     const int E = dtype == NGC_BF16 ? 8 : 4, nvec = cols / E + (cols % E != 0);
     if (cols < E) return {LN_TINY, 1, 1, (int)(((int64_t)rows + 255) / 256)};
-    // {vectors per lane, lanes}.  A workgroup of 1024 has 128 registers a lane, which the backprop's five values per element do not fit.
-    static const int groups[][2] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {4, 64}, {2, 256}, {4, 256}, {4, 512}, {2, 1024}, {4, 1024}};
-    for (const auto &g : groups) {
-        if (nvec > g[0] * g[1] || (bwd ? g[1] == 1024 : g[1] == 512)) continue;
+    // {vectors per lane, lanes}.  The backprop holds five values per element: more than 16 elements a lane leave one wave a SIMD (taken for the
+    // longest rows only), and the 128 registers a lane of a workgroup of 1024 do not hold 16.
+    static const int forward[][2] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {4, 64}, {2, 256}, {4, 256}, {2, 1024}, {4, 1024}, {0, 0}};
+    static const int backprop[][2] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {4, 64}, {1, 256}, {2, 256}, {2, 512}, {4, 512}, {0, 0}};
+    for (const int (*q)[2] = bwd ? backprop : forward; (*q)[0]; ++q) {
+        const int *g = *q;
+        if (nvec > g[0] * g[1] || (bwd && g[0] * E > 16 && g[1] < 512)) continue;
         const int rpw = g[1] <= 64 ? 256 / g[1] : 1, need = (int)(((int64_t)rows + rpw - 1) / rpw);
         // Forward: what the compute units hold at a time.  Backprop: every workgroup leaves 2 cols partial sums, and reads of them cost as much
         // as writes: at most two workgroups of 256 per compute unit, and four rows per group where there are enough rows for that.
@@ -454,30 +463,20 @@ static int norm_parts(int dtype, int rows, int cols)
 
 size_t layer_norm_bwd_workspace(int dtype, int rows, int cols) { return (size_t)norm_parts(dtype, rows, cols) * 2 * cols * sizeof(float); }
 
-#define NGC_LN_REG(KERNEL, ARGS)                                                                                                                   \
-    switch (p.GL * 16 + p.V) {                                                                                                                     \
-    case 8 * 16 + 1: NGC_LAUNCH((KERNEL<T, 1, 8, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                                  \
-    case 16 * 16 + 1: NGC_LAUNCH((KERNEL<T, 1, 16, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                                \
-    case 32 * 16 + 1: NGC_LAUNCH((KERNEL<T, 1, 32, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                                \
-    case 64 * 16 + 1: NGC_LAUNCH((KERNEL<T, 1, 64, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                                \
-    case 64 * 16 + 2: NGC_LAUNCH((KERNEL<T, 2, 64, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                                \
-    case 64 * 16 + 4: NGC_LAUNCH((KERNEL<T, 4, 64, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                                \
-    case 256 * 16 + 2: NGC_LAUNCH((KERNEL<T, 2, 256, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                              \
-    case 256 * 16 + 4: NGC_LAUNCH((KERNEL<T, 4, 256, TAIL>), dim3(p.grid), dim3(256), 0, st, NGC_LN_ARGS ARGS); break;                              \
-    NGC_LN_LONGEST(KERNEL, ARGS)                                                                                                                   \
-    default: return hipErrorInvalidValue;                                                                                                          \
-    }
+#define NGC_LN_CASE(KERNEL, V, GL, ARGS)                                                                                                           \
+    case (GL) * 16 + (V): NGC_LAUNCH((KERNEL<T, V, GL, TAIL>), dim3(p.grid), dim3((GL) <= 64 ? 256 : (GL)), 0, st, NGC_LN_ARGS ARGS); break;
 #define NGC_LN_ARGS(...) __VA_ARGS__
 
 template <typename T, bool TAIL>
 static hipError_t launch_norm_reg(const NormPlan &p, int rows, int cols, float eps, const T *x, const float *gamma, const float *beta, T *y, float *mean,
                                   float *rstd, hipStream_t st)
 {
-#define NGC_LN_LONGEST(KERNEL, ARGS)                                                                                                               \
-    case 1024 * 16 + 2: NGC_LAUNCH((KERNEL<T, 2, 1024, TAIL>), dim3(p.grid), dim3(1024), 0, st, NGC_LN_ARGS ARGS); break;                           \
-    case 1024 * 16 + 4: NGC_LAUNCH((KERNEL<T, 4, 1024, TAIL>), dim3(p.grid), dim3(1024), 0, st, NGC_LN_ARGS ARGS); break;
-    NGC_LN_REG(layer_norm_reg, (x, gamma, beta, y, mean, rstd, rows, cols, eps))
-#undef NGC_LN_LONGEST
+#define NGC_LN(V, GL) NGC_LN_CASE(layer_norm_reg, V, GL, (x, gamma, beta, y, mean, rstd, rows, cols, eps))
+    switch (p.GL * 16 + p.V) {
+        NGC_LN(1, 8) NGC_LN(1, 16) NGC_LN(1, 32) NGC_LN(1, 64) NGC_LN(2, 64) NGC_LN(4, 64) NGC_LN(2, 256) NGC_LN(4, 256) NGC_LN(2, 1024) NGC_LN(4, 1024)
+    default: return hipErrorInvalidValue;
+    }
+#undef NGC_LN
     return launch_result();
 }
 
@@ -485,10 +484,15 @@ template <typename T, bool TAIL>
 static hipError_t launch_norm_bwd_reg(const NormPlan &p, int rows, int cols, const T *x, const float *gamma, const float *mean, const float *rstd,
                                       const T *dy, T *dx, float *part, hipStream_t st)
 {
-#define NGC_LN_LONGEST(KERNEL, ARGS)                                                                                                               \
-    case 512 * 16 + 4: NGC_LAUNCH((KERNEL<T, 4, 512, TAIL>), dim3(p.grid), dim3(512), 0, st, NGC_LN_ARGS ARGS); break;
-    NGC_LN_REG(layer_norm_bwd_reg, (x, gamma, mean, rstd, dy, dx, part, rows, cols))
-#undef NGC_LN_LONGEST
+#define NGC_LN(V, GL) NGC_LN_CASE(layer_norm_bwd_reg, V, GL, (x, gamma, mean, rstd, dy, dx, part, rows, cols))
+    switch (p.GL * 16 + p.V) {
+        NGC_LN(1, 8) NGC_LN(1, 16) NGC_LN(1, 32) NGC_LN(1, 64) NGC_LN(2, 64) NGC_LN(1, 256) NGC_LN(2, 256) NGC_LN(2, 512) NGC_LN(4, 512)
+    case 64 * 16 + 4:
+        if constexpr (sizeof(T) == 4) NGC_LAUNCH((layer_norm_bwd_reg<T, 4, 64, TAIL>), dim3(p.grid), dim3(256), 0, st, x, gamma, mean, rstd, dy, dx, part, rows, cols);
+        break;
+    default: return hipErrorInvalidValue;
+    }
+#undef NGC_LN
     return launch_result();
 }
 

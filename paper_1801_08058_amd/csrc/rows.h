@@ -90,4 +90,12 @@ __device__ __forceinline__ void store16_any(T *p, uint4 v)
     __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any *>(p));
 }
 
+// Vectors that stay packed over several passes: what was unpacked of them before this point is unpacked again after it instead of being kept
+// in registers.
+template <int N> __device__ __forceinline__ void keep_packed(uint4 (&v)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
+}
+
 }  // namespace ngc
