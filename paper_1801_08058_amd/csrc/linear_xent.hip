@@ -4,143 +4,18 @@
 //   g[n][v] = (exp(z[n][v] - lse[n]) - [v = label[n]]) dloss[n],  dx = g w,  dw = g^T x
 //
 // The logits are never kept: the forward pass leaves of every tile the maximum and the sum of each row; the backward pass forms g again
-// for a piece of the vocabulary at a time.
+// for a piece of the vocabulary at a time.  All products run on the bf16 matrix cores (mm_bf16.h); fp32 tensors as three limbs of bf16, which
+// six products of limbs multiply as exactly as fp32 arithmetic does, at a sixth of the bf16 rate: the fp32 matrix instructions have a sixteenth.
 #include "mm_bf16.h"
 #include "rows.h"
+
+#include <stdlib.h>
 
 namespace ngc {
 
 static size_t r256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-// One 64 x 64 tile of c[m][n] = sum_k a(m, k) b(n, k) in fp32; thread (ty, tx) of 16 x 16 holds rows 4 ty .. and columns 4 tx ..
-template <class A, class B>
-__device__ __forceinline__ void tile64(int M, int N, int K, int m0, int n0, A a, B b, float (&acc)[4][4])
-{
-    __shared__ float sa[16][68], sb[16][68];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-    for (int k0 = 0; k0 < K; k0 += 16) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < 1024; e += 256) {
-            const int k = e & 15, r = e >> 4;
-            sa[k][r] = m0 + r < M && k0 + k < K ? a(m0 + r, k0 + k) : 0.f;
-            sb[k][r] = n0 + r < N && k0 + k < K ? b(n0 + r, k0 + k) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += sa[k][4 * ty + i] * sb[k][4 * tx + j];
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void xent_tiles(const T *__restrict__ x, const T *__restrict__ w, const int64_t *__restrict__ labels,
-                                                  float2 *__restrict__ part, float *__restrict__ target, int rows, int width, int vocab)
-{
-    const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4];
-    tile64(rows, vocab, width, m0, n0, [&](int m, int k) { return SmElem<T>::load(x + (size_t)m * width + k); },
-           [&](int n, int k) { return SmElem<T>::load(w + (size_t)n * width + k); }, acc);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = m0 + 4 * ty + i;
-        float top = -INFINITY, s = 0.f;
-        for (int j = 0; j < 4; ++j)
-            if (n0 + 4 * tx + j < vocab) top = fmaxf(top, acc[i][j]);
-        top = group_max<16>(top);
-        for (int j = 0; j < 4; ++j)
-            if (n0 + 4 * tx + j < vocab) s += expf(acc[i][j] - top);
-        s = group_sum<16>(s);
-        if (m >= rows) continue;
-        if (tx == 0) part[(size_t)blockIdx.x * rows + m] = make_float2(top, s);
-        for (int j = 0; j < 4; ++j)
-            if (labels[m] == n0 + 4 * tx + j && labels[m] < vocab) target[m] = acc[i][j];
-    }
-}
-
-__global__ __launch_bounds__(256) void xent_join(const float2 *__restrict__ part, const float *__restrict__ target, const int64_t *__restrict__ labels,
-                                                 float *__restrict__ loss, float *__restrict__ lse, int rows, int vocab, int tiles)
-{
-    const int m = blockIdx.x * 256 + threadIdx.x;
-    if (m >= rows) return;
-    float top = -INFINITY, s = 0.f;
-    for (int t = 0; t < tiles; ++t) top = fmaxf(top, part[(size_t)t * rows + m].x);
-    for (int t = 0; t < tiles; ++t) s += part[(size_t)t * rows + m].y * expf(part[(size_t)t * rows + m].x - top);
-    const float l = top + logf(s);
-    lse[m] = l;
-    loss[m] = labels[m] >= 0 && labels[m] < vocab ? l - target[m] : 0.f;
-}
-
-// g of the piece of the vocabulary from v0 on: [rows][piece]
-template <typename T>
-__global__ __launch_bounds__(256) void xent_grad_tiles(const T *__restrict__ x, const T *__restrict__ w, const int64_t *__restrict__ labels,
-                                                       const float *__restrict__ lse, const float *__restrict__ dloss, float *__restrict__ g, int rows,
-                                                       int width, int vocab, int v0, int piece)
-{
-    const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4];
-    tile64(rows, piece, width, m0, n0, [&](int m, int k) { return SmElem<T>::load(x + (size_t)m * width + k); },
-           [&](int n, int k) { return SmElem<T>::load(w + (size_t)(v0 + n) * width + k); }, acc);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = m0 + 4 * ty + i;
-        if (m >= rows) continue;
-        const int64_t label = labels[m];
-        const bool live = label >= 0 && label < vocab;
-        for (int j = 0; j < 4; ++j) {
-            const int n = n0 + 4 * tx + j;
-            if (n < piece) g[(size_t)m * piece + n] = live ? (expf(acc[i][j] - lse[m]) - (label == v0 + n ? 1.f : 0.f)) * dloss[m] : 0.f;
-        }
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void xent_dx_tiles(const float *__restrict__ g, const T *__restrict__ w, float *__restrict__ dx, int rows, int width,
-                                                     int v0, int piece)
-{
-    const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4];
-    tile64(rows, width, piece, m0, n0, [&](int m, int k) { return g[(size_t)m * piece + k]; },
-           [&](int n, int k) { return SmElem<T>::load(w + (size_t)(v0 + k) * width + n); }, acc);
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + 4 * ty + i, n = n0 + 4 * tx + j;
-            if (m < rows && n < width) dx[(size_t)m * width + n] = acc[i][j] + (v0 ? dx[(size_t)m * width + n] : 0.f);
-        }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void xent_dw_tiles(const float *__restrict__ g, const T *__restrict__ x, T *__restrict__ dw, int rows, int width,
-                                                     int v0, int piece)
-{
-    const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4];
-    tile64(piece, width, rows, m0, n0, [&](int m, int k) { return g[(size_t)k * piece + m]; },
-           [&](int n, int k) { return SmElem<T>::load(x + (size_t)k * width + n); }, acc);
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + 4 * ty + i, n = n0 + 4 * tx + j;
-            if (m < piece && n < width) SmElem<T>::store(dw + (size_t)(v0 + m) * width + n, acc[i][j]);
-        }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void xent_dx_store(const float *__restrict__ sum, T *__restrict__ dx, size_t n)
-{
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) SmElem<T>::store(dx + i, sum[i]);
-}
-
-constexpr int XENT_PIECE = 4096;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-
-// ---- bf16: the products on the matrix cores -------------------------------------------------------------------------------
 
 // What the backward pass needs of a row: lse in units of log 2, dloss over the largest |dloss| (0 for rows that do not count), the label (-1)
 struct XentRow {
@@ -166,6 +41,7 @@ __global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ la
     if (threadIdx.x == 0) *scale = top;
 }
 
+// T: uint16_t (bf16) or float (in limbs)
 enum XentEpilogue { XE_STATS, XE_GRAD, XE_SLAB, XE_OUT };
 
 struct XentMm {
@@ -176,24 +52,25 @@ struct XentMm {
     float *target;                       // STATS
     const XentRow *info;                 // GRAD
     const float *scale;                  // OUT
-    uint16_t *out;                       // GRAD: g, OUT: the result
-    int64_t ldo;
-    int store_n;                         // columns that are stored (GRAD: zeros past the piece)
+    void *out;                           // GRAD: g (bf16; fp32: its limbs, glimb elements apart), OUT: the result
+    int64_t ldo, glimb;
+    int store_m, store_n;                // rows and columns that are stored (GRAD: zeros past the rows and the piece)
     float *slab;                         // SLAB: [splits][M][ldo]
     int add;                             // SLAB: onto what is there
 };
 
-template <int BM, int BN, int WM, int WN, bool AT, bool BT, XentEpilogue E>
+template <typename T, int BM, int BN, int WM, int WN, bool AT, bool BT, XentEpilogue E>
 __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
 {
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr bool LIMBS = sizeof(T) == 4;
     extern __shared__ __align__(16) unsigned char smem[];
     const int tiles = p.mm.mt * p.mm.nt, split = blockIdx.x / tiles;
     int tm, tn;
     mm_tile_of(blockIdx.x - split * tiles, tiles, p.mm.mt, p.mm.nt, tm, tn);
     const int k0 = split * p.mm.kper, k1 = p.mm.K - k0 < p.mm.kper ? p.mm.K : k0 + p.mm.kper;
     mm_f32x4 acc[FN][FM];
-    mm_tile<BM, BN, WM, WN, AT, BT>(p.mm, smem, tm * BM, tn * BN, k0, k1, acc);
+    mm_tile<BM, BN, WM, WN, AT, BT, LIMBS>(p.mm, smem, tm * BM, tn * BN, k0, k1, acc);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     const int wm = (wave % WM) * (BM / WM), wn = (wave / WM) * (BN / WN);
@@ -201,37 +78,42 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
     if constexpr (E == XE_STATS) {
         // a row of the tile: its maximum and sum of exponentials over 4 FN values of a lane, 4 lanes, WN waves
         float2 *red = reinterpret_cast<float2 *>(smem);                          // [WN][BM]
+        auto rows = [&](auto whole) {                                            // whole: no columns past the end, which count nothing
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const int m = m_ + 16 * j;
+                float top = -INFINITY, s = 0.f;
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, whole || n_ + 16 * i + e < p.mm.N ? acc[i][j][e] : -INFINITY);
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64)) * LOG2E;
+                const float t = top == -INFINITY ? 0.f : top;                    // a wave whose columns are all past the end: sum 0
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -t));
+                        s += whole || n_ + 16 * i + e < p.mm.N ? v : 0.f;
+                    }
+                s += __shfl_xor(s, 16, 64);
+                s += __shfl_xor(s, 32, 64);
+                if (g == 0) red[(wave / WM) * BM + wm + 16 * j + lane] = make_float2(top, s);
+            }
+        };
+        if ((tn + 1) * BN <= p.mm.N) rows(std::true_type());
+        else rows(std::false_type());
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
             const int m = m_ + 16 * j;
-            float top = -INFINITY, s = 0.f;
+            const int64_t label = m < p.mm.M ? p.labels[m] - p.v0 : -1;
+            if (label >= tn * BN + wn && label < tn * BN + wn + BN / WN && label < p.mm.N) {
 #pragma unroll
-            for (int i = 0; i < FN; ++i)
+                for (int i = 0; i < FN; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float z = n_ + 16 * i + e < p.mm.N ? acc[i][j][e] * LOG2E : -INFINITY;
-                    top = fmaxf(top, z);
-                }
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float t = top == -INFINITY ? 0.f : top;                        // a wave whose columns are all past the end: sum 0
-#pragma unroll
-            for (int i = 0; i < FN; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    s += n_ + 16 * i + e < p.mm.N ? __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -t)) : 0.f;
-            s += __shfl_xor(s, 16, 64);
-            s += __shfl_xor(s, 32, 64);
-            if (g == 0) red[(wave / WM) * BM + wm + 16 * j + lane] = make_float2(top, s);
-            if (m < p.mm.M) {
-                const int64_t label = p.labels[m] - p.v0;
-                if (label >= tn * BN + wn && label < tn * BN + wn + BN / WN && label < p.mm.N) {
-#pragma unroll
-                    for (int i = 0; i < FN; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (label == n_ + 16 * i + e) p.target[m] = acc[i][j][e];
-                }
+                    for (int e = 0; e < 4; ++e)
+                        if (label == n_ + 16 * i + e) p.target[m] = acc[i][j][e];
             }
         }
         __syncthreads();
@@ -249,48 +131,104 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
     }
     float scale = 1.f;
     if constexpr (E == XE_OUT) scale = *p.scale;
+    const bool whole = (tn + 1) * BN <= p.store_n;
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
         const int m = m_ + 16 * j;
-        if (m >= p.mm.M) continue;
-        XentRow row;
-        if constexpr (E == XE_GRAD) row = p.info[m];
+        if constexpr (E == XE_SLAB) {
+            if (m >= p.store_m) continue;
 #pragma unroll
-        for (int i = 0; i < FN; ++i) {
-            const int n = n_ + 16 * i;
-            mm_f32x4 v = acc[i][j];
-            if constexpr (E == XE_SLAB) {
+            for (int i = 0; i < FN; ++i) {
+                const int n = n_ + 16 * i;
                 if (n >= p.store_n) continue;
                 float *at = p.slab + ((size_t)split * p.mm.M + m) * p.ldo + n;  // ldo and store_n are multiples of 8
+                mm_f32x4 v = acc[i][j];
                 if (p.add) v += *reinterpret_cast<const mm_f32x4 *>(at);
                 *reinterpret_cast<mm_f32x4 *>(at) = v;
-                continue;
             }
-            if constexpr (E == XE_GRAD) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float prob = __builtin_amdgcn_exp2f(fmaf(v[e], LOG2E, -row.lse2));
-                    v[e] = row.label >= 0 && n + e < p.mm.N ? (prob - (row.label == p.v0 + n + e ? 1.f : 0.f)) * row.factor : 0.f;
-                }
-            } else {
-                v *= scale;
-            }
-            uint16_t *at = p.out + (size_t)m * p.ldo + n;
-            const uint32_t lo = pack_bf16x2_hw(v[0], v[1]), hi = pack_bf16x2_hw(v[2], v[3]);
-            if (n + 4 <= p.store_n && (p.ldo & 3) == 0) {
-                *reinterpret_cast<uint2 *>(at) = make_uint2(lo, hi);
-            } else {
-                if (n < p.store_n) at[0] = (uint16_t)lo;
-                if (n + 1 < p.store_n) at[1] = (uint16_t)(lo >> 16);
-                if (n + 2 < p.store_n) at[2] = (uint16_t)hi;
-                if (n + 3 < p.store_n) at[3] = (uint16_t)(hi >> 16);
-            }
+            continue;
         }
+        if constexpr (E == XE_GRAD) {
+            XentRow row = {0.f, 0.f, -1, 0};
+            if (m < p.mm.M) row = p.info[m];
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -row.lse2)) * row.factor;
+            const int label = row.label - p.v0;                                  // few waves hold one
+            if (__any(label >= tn * BN + wn && label < tn * BN + wn + BN / WN)) {
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] -= label == n_ + 16 * i + e ? row.factor : 0.f;
+            }
+            if ((tn + 1) * BN > p.mm.N || __any(row.label < 0)) {                // +0 past the piece and in rows that do not count
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (row.label < 0 || n_ + 16 * i + e >= p.mm.N) acc[i][j][e] = 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < FN; ++i) acc[i][j] *= scale;
+        }
+        if constexpr (E == XE_OUT && LIMBS) {
+            if (m >= p.store_m) continue;
+#pragma unroll
+            for (int i = 0; i < FN; ++i) {
+                const int n = n_ + 16 * i;
+                float *at = static_cast<float *>(p.out) + (size_t)m * p.ldo + n;
+                if (whole || n + 4 <= p.store_n) {
+                    __builtin_memcpy(at, &acc[i][j], 16);                        // any element address
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n + e < p.store_n) at[e] = acc[i][j][e];
+                }
+            }
+            continue;
+        }
+        // bf16: the four lanes of a row exchange quarters of two fragments, so that each has 8 neighbouring columns and a store covers 64 bytes of
+        // the row.  Swapping the upper half wave of the first with the lower of the second gives lane g of fragment g / 2 the quarters g % 2 and
+        // 2 + g % 2, swapping odd and even rows of 16 lanes then the quarters 2 (g % 2) and 2 (g % 2) + 1.
+#pragma unroll
+        for (int i = 0; i < FN; i += 2)
+#pragma unroll
+            for (int l = 0; l < (E == XE_GRAD && LIMBS ? 3 : 1); ++l) {
+                uint32_t q[2][2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    mm_f32x4 &v = acc[i + k][j];
+                    q[k][0] = pack_bf16x2_hw(v[0], v[1]);
+                    q[k][1] = pack_bf16x2_hw(v[2], v[3]);
+                    if (E == XE_GRAD && LIMBS)
+                        v -= mm_f32x4{__uint_as_float(q[k][0] << 16), __uint_as_float(q[k][0] & 0xFFFF0000u), __uint_as_float(q[k][1] << 16), __uint_as_float(q[k][1] & 0xFFFF0000u)};
+                }
+                uint32_t o[4];
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const auto a = __builtin_amdgcn_permlane32_swap(q[0][w], q[1][w], false, false);
+                    const auto b = __builtin_amdgcn_permlane16_swap(a[0], a[1], false, false);
+                    o[w] = b[0];
+                    o[2 + w] = b[1];
+                }
+                const int n = tn * BN + wn + 16 * i + 16 * (g >> 1) + 8 * (g & 1);
+                uint16_t *at = static_cast<uint16_t *>(p.out) + (size_t)m * p.ldo + n + l * p.glimb;
+                if (m >= p.store_m) continue;
+                if (whole || n + 8 <= p.store_n) {
+                    __builtin_memcpy(at, o, 16);                                 // any element address
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (n + e < p.store_n) at[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
+                }
+            }
     }
 }
 
 // lse and loss of 32 rows from the tiles' maxima and sums, eight parts of the tiles each
-__global__ __launch_bounds__(256) void xent_join2(const float2 *__restrict__ part, const float *__restrict__ target, const int64_t *__restrict__ labels,
+__global__ __launch_bounds__(256) void xent_join(const float2 *__restrict__ part, const float *__restrict__ target, const int64_t *__restrict__ labels,
                                                   float *__restrict__ loss, float *__restrict__ lse, int rows, int vocab, int tiles)
 {
     __shared__ float2 red[8][32];
@@ -318,16 +256,30 @@ __global__ __launch_bounds__(256) void xent_join2(const float2 *__restrict__ par
     loss[m] = labels[m] >= 0 && labels[m] < vocab ? l - target[m] : 0.f;
 }
 
-// rows of `width` elements to rows of `pitch` (zeros behind them)
-__global__ __launch_bounds__(256) void xent_pad(const uint16_t *__restrict__ src, uint16_t *__restrict__ dst, int64_t rows, int width, int pitch)
+// Rows of `width` elements as the products read them: of `pitch` elements, zeros behind them and in the rows from `rows` to `all`.  fp32 values
+// become three limbs, `limb` elements apart: the value rounded to bf16, what that leaves, rounded, and what that leaves.
+template <typename T>
+__global__ __launch_bounds__(256) void xent_pad(const T *__restrict__ src, uint16_t *__restrict__ dst, int64_t rows, int64_t all, int width, int pitch,
+                                                int64_t limb)
 {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int j = threadIdx.x; j < pitch; j += 256) dst[(size_t)r * pitch + j] = j < width ? src[(size_t)r * width + j] : (uint16_t)0;
+    for (int64_t r = blockIdx.x; r < all; r += gridDim.x)
+        for (int j = threadIdx.x * 2; j < pitch; j += 512) {                                    // pitch is even
+            float a = r < rows && j < width ? SmElem<T>::load(src + (size_t)r * width + j) : 0.f;
+            float b = r < rows && j + 1 < width ? SmElem<T>::load(src + (size_t)r * width + j + 1) : 0.f;
+#pragma unroll
+            for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
+                const uint32_t q = pack_bf16x2_hw(a, b);
+                *reinterpret_cast<uint32_t *>(dst + l * limb + (size_t)r * pitch + j) = q;
+                a -= __uint_as_float(q << 16);
+                b -= __uint_as_float(q & 0xFFFF0000u);
+            }
+        }
 }
 
 // out[r][j] = scale * sum of the slabs
-__global__ __launch_bounds__(256) void xent_sum(const float *__restrict__ slab, const float *__restrict__ scale, uint16_t *__restrict__ out, int rows,
-                                                int width, int pitch, int splits)
+template <typename T>
+__global__ __launch_bounds__(256) void xent_sum(const float *__restrict__ slab, const float *__restrict__ scale, T *__restrict__ out, int rows, int width,
+                                                int pitch, int splits)
 {
     const int j = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (j >= width) return;
@@ -335,21 +287,20 @@ __global__ __launch_bounds__(256) void xent_sum(const float *__restrict__ slab, 
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
         mm_f32x4 v = mm_f32x4{0.f, 0.f, 0.f, 0.f};
         for (int q = 0; q < splits; ++q) v += *reinterpret_cast<const mm_f32x4 *>(slab + ((size_t)q * rows + r) * pitch + j);
-        for (int e = 0; e < 4 && j + e < width; ++e) out[(size_t)r * width + j + e] = (uint16_t)(pack_bf16x2_hw(v[e] * s, 0.f) & 0xFFFFu);
+        for (int e = 0; e < 4 && j + e < width; ++e) SmElem<T>::store(out + (size_t)r * width + j + e, v[e] * s);
     }
 }
 
-static int up(int v, int to) { return (v + to - 1) / to * to; }
-
-// How a call goes through the vocabulary.  Pieces are as large as 512 MiB of g, and of a padded copy of w, allow.
+// How a call goes through the vocabulary.  Pieces are as large as 512 MiB of g, and of a copy of w, allow.
 struct XentPlan {
-    bool pad;                    // rows of no multiple of 16 bytes, or tensors off that grid, are copied first
-    int pitch, piece;            // elements of a row of x and w as the products read them; classes of a piece
+    bool copy;                   // x and w are copied first: fp32, or rows of no multiple of 16 bytes (tensors off that grid are as well)
+    int limbs, pitch, piece;     // limbs of an element; elements of a row of x and w as the products read them; classes of a piece
+    int64_t krows;               // rows as the products count them where they are the reduction
     int dx_splits, dw_splits;
-    size_t info, scale, xpad, wpad, g, dx_slab, dw_slab, total;         // offsets in the workspace
+    size_t info, scale, xcopy, wcopy, g, dx_slab, dw_slab, total;        // offsets in the workspace
 };
 
-static int splits_for(int64_t tiles, int k)
+static int splits_for(int64_t tiles, int64_t k)
 {
     // parts of at least 512: fewer than half the compute units have a tile otherwise
     int s = 1;
@@ -357,170 +308,175 @@ static int splits_for(int64_t tiles, int k)
     return s;
 }
 static int64_t tiles128(int64_t m, int64_t n) { return ((m + 127) / 128) * ((n + 127) / 128); }
+static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
 
-static XentPlan xent_plan(int64_t rows, int width, int vocab, bool bwd, bool dx, bool dw)
+static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bwd)
 {
     XentPlan p{};
-    p.pitch = up(width, 8);
-    p.pad = p.pitch != width;
-    const int64_t most = (int64_t)512 << 20;
+    p.limbs = dtype == NGC_F32 ? 3 : 1;
+    p.pitch = (int)up(width, p.limbs == 3 ? 32 : 8);
+    p.copy = p.limbs == 3 || p.pitch != width;
+    p.krows = p.limbs == 3 ? up(rows, 32) : rows;
+    const int64_t most = ((int64_t)512 << 20) / 2 / p.limbs;             // elements
     int64_t piece = vocab;
-    if (bwd) piece = piece < most / 2 / rows ? piece : most / 2 / rows;
-    piece = piece < most / 2 / p.pitch ? piece : most / 2 / p.pitch;
-    p.piece = (int)(piece < vocab ? (piece / 256 > 0 ? piece / 256 * 256 : 256) : vocab);
-    p.dx_splits = dx ? splits_for(tiles128(rows, width), p.piece) : 1;
-    p.dw_splits = dw ? splits_for(tiles128(p.piece, width), (int)rows) : 1;
-    return p;
-}
-
-static size_t xent_lay_out(XentPlan &p, int64_t rows, int vocab, bool bwd)
-{
+    if (bwd && piece > most / p.krows) piece = most / p.krows;
+    if (piece > most / p.pitch) piece = most / p.pitch;
+    p.piece = (int)(piece >= vocab ? vocab : piece < 256 ? 256 : piece / 256 * 256);
+    if (p.piece > vocab) p.piece = vocab;
+    p.dx_splits = splits_for(tiles128(rows, width), p.piece);
+    p.dw_splits = splits_for(tiles128(p.piece, width), rows);
     size_t at = 0;
     auto take = [&](size_t &where, size_t bytes) { where = at; at += r256(bytes); };
     if (!bwd) {
-        take(p.info, (size_t)rows * 8 * ((size_t)(vocab + 63) / 64 + (vocab + p.piece - 1) / p.piece));      // part
-        take(p.scale, (size_t)rows * 4);                                                                    // target
+        take(p.info, (size_t)rows * 8 * ((size_t)((int64_t)vocab + 63) / 64 + (vocab - 1) / p.piece + 1));       // part
+        take(p.scale, (size_t)rows * 4);                                                                        // target
     } else {
         take(p.info, (size_t)rows * sizeof(XentRow));
         take(p.scale, 4);
-        take(p.g, (size_t)rows * up(p.piece, 64) * 2);
+        take(p.g, (size_t)p.krows * up(p.piece, 64) * 2 * p.limbs);
         take(p.dx_slab, (size_t)rows * p.pitch * 4 * p.dx_splits);
         take(p.dw_slab, p.dw_splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw_splits : 0);
     }
-    take(p.xpad, (size_t)rows * p.pitch * 2);
-    take(p.wpad, (size_t)p.piece * p.pitch * 2);
+    take(p.xcopy, (size_t)p.krows * p.pitch * 2 * p.limbs);
+    take(p.wcopy, (size_t)up(p.piece, 32) * p.pitch * 2 * p.limbs);
     p.total = at;
-    return at;
+    return p;
 }
 
-template <int BM, int BN, int WM, int WN, bool AT, bool BT, XentEpilogue E>
+template <typename T, int BM, int BN, int WM, int WN, bool AT, bool BT, XentEpilogue E>
 static hipError_t launch_mm_tile(XentMm p, hipStream_t st)
 {
     static LdsLimitOnce lds;
-    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<BM, BN, WM, WN, AT, BT, E>));
+    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<T, BM, BN, WM, WN, AT, BT, E>));
     if (e != hipSuccess) return e;
     p.mm.mt = (p.mm.M + BM - 1) / BM;
     p.mm.nt = (p.mm.N + BN - 1) / BN;
-    p.mm.kper = up((p.mm.K + p.mm.splits - 1) / p.mm.splits, 32);
-    NGC_LAUNCH((xent_mm<BM, BN, WM, WN, AT, BT, E>), dim3((unsigned)(p.mm.mt * p.mm.nt * p.mm.splits)), dim3(64 * WM * WN), (mm_lds_bytes<BM, BN>()), st, p);
+    p.mm.kper = (int)up((p.mm.K + p.mm.splits - 1) / p.mm.splits, 32);
+    NGC_LAUNCH((xent_mm<T, BM, BN, WM, WN, AT, BT, E>), dim3((unsigned)(p.mm.mt * p.mm.nt * p.mm.splits)), dim3(64 * WM * WN), (mm_lds_bytes<BM, BN>()), st, p);
     return launch_result();
 }
 
 // The largest tile that still gives most compute units one
 static int mm_tile_size(int64_t m, int64_t n, int splits)
 {
+    if (const char *v = env_switch(SW_XENT_TILE)) return atoi(v);
     if (((m + 255) / 256) * ((n + 255) / 256) * splits >= 192) return 256;
     if (tiles128(m, n) * splits >= 128) return 128;
     return 64;
 }
 
-template <bool AT, bool BT, XentEpilogue E>
+template <typename T, bool AT, bool BT, XentEpilogue E>
 static hipError_t launch_mm(const XentMm &p, int tile, hipStream_t st)
 {
-    if (tile == 256) return launch_mm_tile<256, 256, 2, 2, AT, BT, E>(p, st);
-    if (tile == 128) return launch_mm_tile<128, 128, 2, 2, AT, BT, E>(p, st);
-    return launch_mm_tile<64, 64, 2, 2, AT, BT, E>(p, st);
+    if (tile == 256) return launch_mm_tile<T, 256, 256, 2, 2, AT, BT, E>(p, st);
+    if (tile == 128) return launch_mm_tile<T, 128, 128, 2, 2, AT, BT, E>(p, st);
+    return launch_mm_tile<T, 64, 64, 2, 2, AT, BT, E>(p, st);
 }
 
-static hipError_t pad_rows(const uint16_t *src, uint16_t *dst, int64_t rows, int width, int pitch, hipStream_t st)
+// x or rows of w as the products read them: where they are, or a copy.  all: rows of the copy
+template <typename T>
+static hipError_t operand(const XentPlan &pl, const T *src, char *copy, int64_t rows, int64_t all, int width, const uint16_t *&out, hipStream_t st)
 {
-    NGC_LAUNCH(xent_pad, dim3((unsigned)(rows < 65536 ? rows : 65536)), dim3(256), 0, st, src, dst, rows, width, pitch);
+    out = reinterpret_cast<const uint16_t *>(src);
+    if (!pl.copy && (reinterpret_cast<uintptr_t>(src) & 15) == 0) return hipSuccess;
+    out = reinterpret_cast<const uint16_t *>(copy);
+    NGC_LAUNCH((xent_pad<T>), dim3((unsigned)(all < 65536 ? all : 65536)), dim3(256), 0, st, src, reinterpret_cast<uint16_t *>(copy), rows, all, width, pl.pitch,
+               all * pl.pitch);
     return launch_result();
 }
 
-static bool on_grid(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-static hipError_t launch_xent_bf16(int rows, int width, int vocab, const uint16_t *x, const uint16_t *w, const int64_t *labels, float *loss, float *lse,
-                                   char *ws, hipStream_t st)
+template <typename T>
+static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, const T *w, const int64_t *labels, float *loss, float *lse, char *ws, hipStream_t st)
 {
-    XentPlan pl = xent_plan(rows, width, vocab, false, false, false);
-    xent_lay_out(pl, rows, vocab, false);
-    const bool pad_x = pl.pad || !on_grid(x), pad_w = pl.pad || !on_grid(w);
-    hipError_t e;
-    if (pad_x && (e = pad_rows(x, reinterpret_cast<uint16_t *>(ws + pl.xpad), rows, width, pl.pitch, st)) != hipSuccess) return e;
+    const XentPlan pl = xent_plan(sizeof(T) == 4 ? NGC_F32 : NGC_BF16, rows, width, vocab, false);
+    const bool copy_w = pl.copy || (reinterpret_cast<uintptr_t>(w) & 15) != 0;
+    XentMm p{};
+    hipError_t e = operand(pl, x, ws + pl.xcopy, rows, rows, width, p.mm.a, st);
+    if (e != hipSuccess) return e;
+    p.mm.lda = p.mm.ldb = pl.pitch;
+    p.mm.M = rows; p.mm.K = pl.pitch; p.mm.splits = 1;
+    p.mm.alimb = (int64_t)rows * pl.pitch;
+    p.vocab = vocab; p.labels = labels;
+    p.target = reinterpret_cast<float *>(ws + pl.scale);
+    float2 *part = reinterpret_cast<float2 *>(ws + pl.info);
     int tiles = 0;
-    for (int v0 = 0, piece; v0 < vocab; v0 += piece) {
-        piece = pad_w ? (vocab - v0 < pl.piece ? vocab - v0 : pl.piece) : vocab;
-        const uint16_t *wp = w + (size_t)v0 * width;
-        if (pad_w) {
-            if ((e = pad_rows(wp, reinterpret_cast<uint16_t *>(ws + pl.wpad), piece, width, pl.pitch, st)) != hipSuccess) return e;
-            wp = reinterpret_cast<uint16_t *>(ws + pl.wpad);
-        }
-        XentMm p{};
-        p.mm.a = pad_x ? reinterpret_cast<uint16_t *>(ws + pl.xpad) : x;
-        p.mm.b = wp;
-        p.mm.lda = p.mm.ldb = pl.pitch;
-        p.mm.M = rows; p.mm.N = piece; p.mm.K = pl.pitch; p.mm.splits = 1;
-        p.v0 = v0; p.vocab = vocab; p.labels = labels;
-        p.part = reinterpret_cast<float2 *>(ws + pl.info) + (size_t)tiles * rows;
-        p.target = reinterpret_cast<float *>(ws + pl.scale);
-        const int tile = mm_tile_size(rows, piece, 1);
-        if ((e = launch_mm<false, false, XE_STATS>(p, tile, st)) != hipSuccess) return e;
-        tiles += (piece + tile - 1) / tile;
+    for (int64_t v0 = 0; v0 < vocab; v0 += p.mm.N) {
+        const int64_t left = vocab - v0;
+        p.mm.N = (int)(!copy_w || left < pl.piece ? left : pl.piece);    // only copies make pieces
+        if ((e = operand(pl, w + (size_t)v0 * width, ws + pl.wcopy, p.mm.N, p.mm.N, width, p.mm.b, st)) != hipSuccess) return e;
+        p.mm.blimb = (int64_t)p.mm.N * pl.pitch;
+        p.v0 = (int)v0;
+        p.part = part + (size_t)tiles * rows;
+        const int tile = mm_tile_size(rows, p.mm.N, 1);
+        if ((e = launch_mm<T, false, false, XE_STATS>(p, tile, st)) != hipSuccess) return e;
+        tiles += (p.mm.N + tile - 1) / tile;
     }
-    NGC_LAUNCH(xent_join2, dim3((rows + 31) / 32), dim3(256), 0, st, reinterpret_cast<float2 *>(ws + pl.info), reinterpret_cast<float *>(ws + pl.scale), labels,
-               loss, lse, rows, vocab, tiles);
+    NGC_LAUNCH(xent_join, dim3((rows + 31) / 32), dim3(256), 0, st, part, p.target, labels, loss, lse, rows, vocab, tiles);
     return launch_result();
 }
 
-static hipError_t sum_slabs(const float *slab, const float *scale, uint16_t *out, int rows, int width, int pitch, int splits, hipStream_t st)
+template <typename T>
+static hipError_t sum_slabs(const float *slab, const float *scale, T *out, int rows, int width, int pitch, int splits, hipStream_t st)
 {
-    NGC_LAUNCH(xent_sum, dim3((width + 1023) / 1024, rows < 32768 ? rows : 32768), dim3(256), 0, st, slab, scale, out, rows, width, pitch, splits);
+    NGC_LAUNCH((xent_sum<T>), dim3((unsigned)(((int64_t)width + 1023) / 1024), rows < 32768 ? rows : 32768), dim3(256), 0, st, slab, scale, out, rows, width,
+               pitch, splits);
     return launch_result();
 }
 
-static hipError_t launch_xent_bwd_bf16(int rows, int width, int vocab, const uint16_t *x, const uint16_t *w, const int64_t *labels, const float *lse,
-                                       const float *dloss, uint16_t *dx, uint16_t *dw, char *ws, hipStream_t st)
+template <typename T>
+static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, const T *w, const int64_t *labels, const float *lse, const float *dloss,
+                                    T *dx, T *dw, char *ws, hipStream_t st)
 {
-    XentPlan pl = xent_plan(rows, width, vocab, true, true, true);
-    xent_lay_out(pl, rows, vocab, true);
+    const XentPlan pl = xent_plan(sizeof(T) == 4 ? NGC_F32 : NGC_BF16, rows, width, vocab, true);
     XentRow *info = reinterpret_cast<XentRow *>(ws + pl.info);
     float *scale = reinterpret_cast<float *>(ws + pl.scale), *dx_slab = reinterpret_cast<float *>(ws + pl.dx_slab), *dw_slab = reinterpret_cast<float *>(ws + pl.dw_slab);
-    uint16_t *g = reinterpret_cast<uint16_t *>(ws + pl.g);
-    const bool pad_x = pl.pad || !on_grid(x), pad_w = pl.pad || !on_grid(w);
     hipError_t e;
     NGC_LAUNCH(xent_rows, dim3(1), dim3(1024), 0, st, labels, lse, dloss, info, scale, rows, vocab);
     if ((e = launch_result()) != hipSuccess) return e;
-    if (pad_x && (e = pad_rows(x, reinterpret_cast<uint16_t *>(ws + pl.xpad), rows, width, pl.pitch, st)) != hipSuccess) return e;
-    const uint16_t *xp = pad_x ? reinterpret_cast<uint16_t *>(ws + pl.xpad) : x;
-    const bool one = pl.piece >= vocab && pl.dx_splits == 1;
-    for (int v0 = 0; v0 < vocab; v0 += pl.piece) {
-        const int piece = vocab - v0 < pl.piece ? vocab - v0 : pl.piece, gp = up(piece, 64);
-        const uint16_t *wp = w + (size_t)v0 * width;
-        if (pad_w) {
-            if ((e = pad_rows(wp, reinterpret_cast<uint16_t *>(ws + pl.wpad), piece, width, pl.pitch, st)) != hipSuccess) return e;
-            wp = reinterpret_cast<uint16_t *>(ws + pl.wpad);
-        }
+    const uint16_t *xp, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
+    if ((e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
+    const bool one = pl.piece >= vocab && pl.dx_splits == 1;             // dx leaves the products whole
+    for (int64_t v0 = 0; v0 < vocab; v0 += pl.piece) {
+        const int piece = vocab - v0 < pl.piece ? (int)(vocab - v0) : pl.piece, gp = (int)up(piece, 64);
+        const int kpiece = (int)(pl.limbs == 3 ? up(piece, 32) : piece);
+        if ((e = operand(pl, w + (size_t)v0 * width, ws + pl.wcopy, piece, kpiece, width, wp, st)) != hipSuccess) return e;
         XentMm p{};
-        p.v0 = v0; p.vocab = vocab; p.info = info; p.scale = scale;
-        p.mm.a = xp; p.mm.b = wp; p.mm.lda = p.mm.ldb = pl.pitch;
+        p.v0 = (int)v0; p.vocab = vocab; p.info = info; p.scale = scale;
+        p.mm.a = xp; p.mm.b = wp;
+        p.mm.lda = p.mm.ldb = pl.pitch;
+        p.mm.alimb = pl.krows * pl.pitch; p.mm.blimb = (int64_t)kpiece * pl.pitch;
         p.mm.M = rows; p.mm.N = piece; p.mm.K = pl.pitch; p.mm.splits = 1;
-        p.out = g; p.ldo = gp; p.store_n = gp;
-        if ((e = launch_mm<false, false, XE_GRAD>(p, mm_tile_size(rows, piece, 1), st)) != hipSuccess) return e;
+        p.out = ws + pl.g; p.ldo = gp; p.glimb = pl.krows * gp; p.store_m = (int)pl.krows; p.store_n = gp;
+        if ((e = launch_mm<T, false, false, XE_GRAD>(p, mm_tile_size(rows, piece, 1), st)) != hipSuccess) return e;
         if (dx) {
             XentMm q = p;
-            q.mm.a = g; q.mm.lda = gp; q.mm.M = rows; q.mm.N = pl.pitch; q.mm.K = piece; q.mm.splits = pl.dx_splits;
+            q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
+            q.mm.M = rows; q.mm.N = pl.pitch; q.mm.K = kpiece; q.mm.splits = pl.dx_splits;
+            q.store_m = rows;
             const int tile = mm_tile_size(rows, width, pl.dx_splits);
             if (one) {
                 q.out = dx; q.ldo = width; q.store_n = width;
-                e = launch_mm<false, true, XE_OUT>(q, tile, st);
+                e = launch_mm<T, false, true, XE_OUT>(q, tile, st);
             } else {
                 q.slab = dx_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = v0 > 0;
-                e = launch_mm<false, true, XE_SLAB>(q, tile, st);
+                e = launch_mm<T, false, true, XE_SLAB>(q, tile, st);
             }
             if (e != hipSuccess) return e;
         }
         if (dw) {
             XentMm q = p;
-            q.mm.a = g; q.mm.lda = gp; q.mm.b = xp; q.mm.M = piece; q.mm.N = pl.pitch; q.mm.K = rows; q.mm.splits = pl.dw_splits;
+            q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
+            q.mm.b = xp; q.mm.blimb = pl.krows * pl.pitch;
+            q.mm.M = piece; q.mm.N = pl.pitch; q.mm.K = (int)pl.krows; q.mm.splits = pl.dw_splits;
+            q.store_m = piece;
             const int tile = mm_tile_size(piece, width, pl.dw_splits);
-            uint16_t *out = dw + (size_t)v0 * width;
+            T *out = dw + (size_t)v0 * width;
             if (pl.dw_splits == 1) {
                 q.out = out; q.ldo = width; q.store_n = width;
-                e = launch_mm<true, true, XE_OUT>(q, tile, st);
+                e = launch_mm<T, true, true, XE_OUT>(q, tile, st);
             } else {
                 q.slab = dw_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = 0;
-                e = launch_mm<true, true, XE_SLAB>(q, tile, st);
+                e = launch_mm<T, true, true, XE_SLAB>(q, tile, st);
                 if (e == hipSuccess) e = sum_slabs(dw_slab, scale, out, piece, width, pl.pitch, pl.dw_splits, st);
             }
             if (e != hipSuccess) return e;
@@ -529,68 +485,24 @@ static hipError_t launch_xent_bwd_bf16(int rows, int width, int vocab, const uin
     return dx && !one ? sum_slabs(dx_slab, scale, dx, rows, width, pl.pitch, pl.dx_splits, st) : hipSuccess;
 }
 
-size_t linear_xent_workspace(int dtype, int64_t rows, int width, int vocab, bool bwd)
-{
-    if (dtype == NGC_BF16) {
-        XentPlan p = xent_plan(rows, width, vocab, bwd, true, true);
-        return xent_lay_out(p, rows, vocab, bwd);
-    }
-    const size_t tiles = ((size_t)vocab + 63) / 64, piece = vocab < XENT_PIECE ? vocab : XENT_PIECE;
-    return bwd ? r256((size_t)rows * piece * 4) + r256((size_t)rows * width * 4) : r256((size_t)rows * tiles * 8) + r256((size_t)rows * 4);
-}
-
-template <typename T>
-static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, const T *w, const int64_t *labels, float *loss, float *lse, void *ws,
-                                hipStream_t st)
-{
-    const int tiles = (vocab + 63) / 64;
-    float2 *part = static_cast<float2 *>(ws);
-    float *target = reinterpret_cast<float *>(static_cast<char *>(ws) + r256((size_t)rows * tiles * 8));
-    NGC_LAUNCH((xent_tiles<T>), dim3(tiles, (rows + 63) / 64), dim3(256), 0, st, x, w, labels, part, target, rows, width, vocab);
-    const hipError_t e = launch_result();
-    if (e != hipSuccess) return e;
-    NGC_LAUNCH(xent_join, dim3((rows + 255) / 256), dim3(256), 0, st, part, target, labels, loss, lse, rows, vocab, tiles);
-    return launch_result();
-}
-
-template <typename T>
-static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, const T *w, const int64_t *labels, const float *lse,
-                                    const float *dloss, T *dx, T *dw, void *ws, hipStream_t st)
-{
-    const int most = vocab < XENT_PIECE ? vocab : XENT_PIECE;
-    float *g = static_cast<float *>(ws), *sum = reinterpret_cast<float *>(static_cast<char *>(ws) + r256((size_t)rows * most * 4));
-    const unsigned mt = (rows + 63) / 64, dt = (width + 63) / 64;
-    for (int v0 = 0; v0 < vocab; v0 += most) {
-        const int piece = vocab - v0 < most ? vocab - v0 : most;
-        NGC_LAUNCH((xent_grad_tiles<T>), dim3((piece + 63) / 64, mt), dim3(256), 0, st, x, w, labels, lse, dloss, g, rows, width, vocab, v0, piece);
-        hipError_t e = launch_result();
-        if (e != hipSuccess) return e;
-        if (dx) NGC_LAUNCH((xent_dx_tiles<T>), dim3(dt, mt), dim3(256), 0, st, g, w, sum, rows, width, v0, piece);
-        if ((e = launch_result()) != hipSuccess) return e;
-        if (dw) NGC_LAUNCH((xent_dw_tiles<T>), dim3(dt, (piece + 63) / 64), dim3(256), 0, st, g, x, dw, rows, width, v0, piece);
-        if ((e = launch_result()) != hipSuccess) return e;
-    }
-    const size_t n = (size_t)rows * width;
-    if (dx) NGC_LAUNCH((xent_dx_store<T>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, sum, dx, n);
-    return launch_result();
-}
+size_t linear_xent_workspace(int dtype, int64_t rows, int width, int vocab, bool bwd) { return xent_plan(dtype, rows, width, vocab, bwd).total; }
 
 hipError_t launch_linear_xent(int dtype, int rows, int width, int vocab, const void *x, const void *w, const int64_t *labels, float *loss, float *lse,
                               void *ws, hipStream_t st)
 {
     if (dtype == NGC_BF16)
-        return launch_xent_bf16(rows, width, vocab, static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(w), labels, loss, lse, static_cast<char *>(ws), st);
-    return launch_xent_t(rows, width, vocab, static_cast<const float *>(x), static_cast<const float *>(w), labels, loss, lse, ws, st);
+        return launch_xent_t(rows, width, vocab, static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(w), labels, loss, lse, static_cast<char *>(ws), st);
+    return launch_xent_t(rows, width, vocab, static_cast<const float *>(x), static_cast<const float *>(w), labels, loss, lse, static_cast<char *>(ws), st);
 }
 
 hipError_t launch_linear_xent_bwd(int dtype, int rows, int width, int vocab, const void *x, const void *w, const int64_t *labels, const float *lse,
                                   const float *dloss, void *dx, void *dw, void *ws, hipStream_t st)
 {
     if (dtype == NGC_BF16)
-        return launch_xent_bwd_bf16(rows, width, vocab, static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(w), labels, lse, dloss,
-                                    static_cast<uint16_t *>(dx), static_cast<uint16_t *>(dw), static_cast<char *>(ws), st);
+        return launch_xent_bwd_t(rows, width, vocab, static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(w), labels, lse, dloss,
+                                 static_cast<uint16_t *>(dx), static_cast<uint16_t *>(dw), static_cast<char *>(ws), st);
     return launch_xent_bwd_t(rows, width, vocab, static_cast<const float *>(x), static_cast<const float *>(w), labels, lse, dloss,
-                             static_cast<float *>(dx), static_cast<float *>(dw), ws, st);
+                             static_cast<float *>(dx), static_cast<float *>(dw), static_cast<char *>(ws), st);
 }
 
 }  // namespace ngc

@@ -8,7 +8,9 @@
 // to registers and the stage NS ahead is asked for: one barrier and one counted wait per stage.
 //
 // LDS of a stage, in units of 16 bytes so that 64 lanes fill 1 KB in lane order:
-//   [R][K] operands   rows of 64 bytes; chunk c of row r sits at c ^ (r / 4 % 4): 16 rows at one chunk touch every bank once
+//   [R][K] operands   rows of 64 bytes; chunk c of row r sits at c ^ (0 or 3 for r / 8 % 2 = 0 or 1).  ds_read_b128 takes lanes 0-3, 12-15, 20-23
+//                     and 24-27 in one cycle, 4-11, 16-19 and 28-31 in the next: rows and chunks that touch every bank once.  (With
+//                     c ^ (r / 4 % 4), which 16 lanes in a row would need, half of the LDS cycles were bank conflicts.)
 //   [K][R] operands   blocks of 8 k x 64 columns, rows of 128 bytes; the 32-byte piece b of a row k sits at b ^ (k / 2 % 2) ^ 2 (k / 8 % 2), and
 //                     ds_read_b64_tr_b16 turns 4 k x 16 columns into four k of one column per lane: two lane groups touch every bank once
 // Rows and k past the ends are read as zeros: lanes whose offset is past the range of the buffer descriptor.
@@ -31,11 +33,18 @@ constexpr unsigned MM_OOB = 0x80000000u;
 struct MmParams {
     const uint16_t *a, *b;
     int64_t lda, ldb;            // elements between rows as stored, multiples of 8; a, b on the 16-byte grid
-    // K: rows of a [K][.] operand past it are not read; a [.][K] operand is read in whole groups of 8, and what lies behind K there has to be
-    // zero.  M / N of an operand that is stored [K][.]: a multiple of 8.
+    // K: rows of a [K][.] operand past it are not read.  Rows are read in whole groups of 8 elements: what a [.][K] operand holds behind K up to
+    // there has to be zero, and a [K][.] operand has to hold something behind M or N.
     int M, N, K;
     int mt, nt, splits, kper;    // tiles; parts of the reduction and their length (a multiple of 32)
+    int64_t alimb, blimb;        // LIMBS: elements between the limbs of an operand; K is a multiple of 32 then
 };
+
+// LIMBS: fp32 operands as sums of three bf16 limbs, 8 significant bits each.  Of the nine products of limbs the six that reach 2^-24 of the
+// result are formed, one after the other along the reduction: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0).
+constexpr int MM_PAIRS = 6;
+__device__ __forceinline__ int mm_limb_a(int pair) { return pair == 5 ? 2 : (pair >> 1) & ~(pair >> 2) & 1; }
+__device__ __forceinline__ int mm_limb_b(int pair) { return pair == 4 ? 2 : pair & 1 & ~(pair >> 2); }
 
 template <int R, bool T, int NW>
 struct MmOperand {
@@ -56,7 +65,7 @@ struct MmOperand {
     __device__ static __forceinline__ int kin(int i, int wave)
     {
         const int lane = threadIdx.x & 63, q = i * NW + wave;
-        return T ? 8 * (q / (R / 64)) + (lane >> 3) : 8 * ((lane & 3) ^ ((rin(i, wave) >> 2) & 3));
+        return T ? 8 * (q / (R / 64)) + (lane >> 3) : 8 * ((lane & 3) ^ ((rin(i, wave) >> 3) & 1 ? 3 : 0));
     }
     __device__ __forceinline__ void init(const uint16_t *p, int64_t ld, int r0, int extent, int k0, int wave)
     {
@@ -79,7 +88,7 @@ struct MmOperand {
         const unsigned v = FULL || kin(i, wave) < kleft ? voff[i] : MM_OOB;
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + (unsigned)(i * NW + wave) * 1024u), "v"(v), "s"(rs));
     }
-    __device__ __forceinline__ void next() { base += step; }
+    __device__ __forceinline__ void next(int64_t more) { base += step + more; }
 };
 
 // this lane's part of the operand of 16 rows / columns: k 8 (lane / 16) .. + 7
@@ -96,7 +105,7 @@ struct MmFragments {
                 at[b] = (unsigned)(g * (R / 64) * 1024 + (r0 >> 6) * 1024 + i * 128 + (((((r0 >> 4) + b) & 3) ^ key) << 5) + (l & 3) * 8 +
                                    ((((r0 >> 4) & 3) + b) >> 2) * 1024);
         } else {
-            at[0] = (unsigned)((r0 + l) * 64 + ((g ^ (l >> 2)) << 4));
+            at[0] = (unsigned)((r0 + l) * 64 + ((g ^ (l >> 3 ? 3 : 0)) << 4));
         }
     }
     __device__ __forceinline__ mm_bf16x8 read(const unsigned char *lds, int f) const
@@ -112,29 +121,15 @@ struct MmFragments {
     }
 };
 
-constexpr int MM_STAGES = 4;
+constexpr int MM_STAGES = 5;
 template <int BM, int BN> constexpr int mm_lds_bytes() { return MM_STAGES * (BM + BN) * 64; }
 
-// acc[j] += b a[j]^T for the FM fragments of a row.  Written out so that the accumulators stay where they are: 256 of them fill the
-// accumulation registers, and the compiler moves them about instead of updating them in place.  The leading wait is the one a matrix
-// instruction needs behind a vector instruction that wrote an operand; mm_settle is the one in front of the first read of a result.
-template <int FM>
-__device__ __forceinline__ void mm_row(mm_f32x4 (&acc)[FM], const mm_bf16x8 &b, const mm_bf16x8 (&a)[FM])
+// Two products, c0 += b a0^T and c1 += b a1^T.  Written out so that the accumulators stay where they are: 256 of them fill the accumulation
+// registers, and the compiler moves them about instead of updating them in place.  The leading wait is the one a matrix instruction needs behind
+// a vector instruction that wrote an operand; mm_settle is the one in front of the first read of a result.
+__device__ __forceinline__ void mm_pair(mm_f32x4 &c0, mm_f32x4 &c1, const mm_bf16x8 &b, const mm_bf16x8 &a0, const mm_bf16x8 &a1)
 {
-#define NGC_MFMA "v_mfma_f32_16x16x32_bf16 "
-    if constexpr (FM == 8)
-        asm volatile("s_nop 1\n\t" NGC_MFMA "%0, %8, %9, %0\n\t" NGC_MFMA "%1, %8, %10, %1\n\t" NGC_MFMA "%2, %8, %11, %2\n\t" NGC_MFMA "%3, %8, %12, %3\n\t"
-                     NGC_MFMA "%4, %8, %13, %4\n\t" NGC_MFMA "%5, %8, %14, %5\n\t" NGC_MFMA "%6, %8, %15, %6\n\t" NGC_MFMA "%7, %8, %16, %7"
-                     : "+a"(acc[0]), "+a"(acc[1]), "+a"(acc[2]), "+a"(acc[3]), "+a"(acc[4]), "+a"(acc[5]), "+a"(acc[6]), "+a"(acc[7])
-                     : "v"(b), "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]));
-    else if constexpr (FM == 4)
-        asm volatile("s_nop 1\n\t" NGC_MFMA "%0, %4, %5, %0\n\t" NGC_MFMA "%1, %4, %6, %1\n\t" NGC_MFMA "%2, %4, %7, %2\n\t" NGC_MFMA "%3, %4, %8, %3"
-                     : "+a"(acc[0]), "+a"(acc[1]), "+a"(acc[2]), "+a"(acc[3])
-                     : "v"(b), "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]));
-    else
-        asm volatile("s_nop 1\n\t" NGC_MFMA "%0, %2, %3, %0\n\t" NGC_MFMA "%1, %2, %4, %1" : "+a"(acc[0]), "+a"(acc[1]) : "v"(b), "v"(a[0]), "v"(a[1]));
-    static_assert(FM == 8 || FM == 4 || FM == 2, "fragments of a row");
-#undef NGC_MFMA
+    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %2, %3, %0\n\tv_mfma_f32_16x16x32_bf16 %1, %2, %4, %1" : "+a"(c0), "+a"(c1) : "v"(b), "v"(a0), "v"(a1));
 }
 template <int FN, int FM>
 __device__ __forceinline__ void mm_settle(mm_f32x4 (&acc)[FN][FM])
@@ -158,7 +153,7 @@ __device__ __forceinline__ void mm_tile_of(int id, int total, int mt, int nt, in
 }
 
 // acc[fn][fm]: n = 16 fn + 4 (lane / 16) + element, m = 16 fm + lane % 16 of the wave's part
-template <int BM, int BN, int WM, int WN, bool AT, bool BT>
+template <int BM, int BN, int WM, int WN, bool AT, bool BT, bool LIMBS>
 __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, int m0, int n0, int k0, int k1, mm_f32x4 (&acc)[BN / WN / 16][BM / WM / 16])
 {
     constexpr int NW = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, STAGE = (BM + BN) * 64, NS = MM_STAGES;
@@ -172,9 +167,25 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
     MmFragments<BN, BT> rb;
     ra.init((wave % WM) * (BM / WM), lane);
     rb.init((wave / WM) * (BN / WN), lane);
-    const int steps = (k1 - k0 + 31) / 32, full = (k1 - k0) / 32;
+    const int per = (k1 - k0 + 31) / 32, steps = LIMBS ? MM_PAIRS * per : per, full = LIMBS ? steps : (k1 - k0) / 32;
+    int asked = 0, pair = 0;                                                 // LIMBS: stages of this pair that were asked for
+    auto advance = [&] {
+        int64_t more_a = 0, more_b = 0;
+        if constexpr (LIMBS) {
+            const bool wrap = ++asked == per;
+            const int64_t ja = 2 * (mm_limb_a(pair + 1) - mm_limb_a(pair)) * p.alimb - (int64_t)per * la.step;
+            const int64_t jb = 2 * (mm_limb_b(pair + 1) - mm_limb_b(pair)) * p.blimb - (int64_t)per * lb.step;
+            more_a = wrap ? ja : 0;
+            more_b = wrap ? jb : 0;
+            pair += wrap ? 1 : 0;
+            asked = wrap ? 0 : asked;
+        }
+        la.next(more_a);
+        lb.next(more_b);
+    };
     const unsigned ring = (unsigned)(uintptr_t)(mm_lds_void *)smem;          // LDS address
     constexpr int LA = MmOperand<BM, AT, NW>::LOADS, LB = MmOperand<BN, BT, NW>::LOADS;
+    constexpr int GAPS = FN * FM / 2, READ_GAPS = GAPS * 3 / 4 > 0 ? GAPS * 3 / 4 : 1;
     mm_bf16x8 fa[2][FM], fb[2][FN];
 #pragma unroll
     for (int i = 0; i < FN; ++i)
@@ -182,13 +193,12 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
         for (int j = 0; j < FM; ++j) acc[i][j] = mm_f32x4{0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < NS && s < steps; ++s) {
 #pragma unroll
-        for (int i = 0; i < LA; ++i) la.template load<false>(i, ring + s * STAGE, wave, k1 - k0 - 32 * s);
+        for (int i = 0; i < LA; ++i) la.template load<LIMBS>(i, ring + s * STAGE, wave, k1 - k0 - 32 * s);
 #pragma unroll
-        for (int i = 0; i < LB; ++i) lb.template load<false>(i, ring + s * STAGE + BM * 64, wave, k1 - k0 - 32 * s);
-        la.next();
-        lb.next();
+        for (int i = 0; i < LB; ++i) lb.template load<LIMBS>(i, ring + s * STAGE + BM * 64, wave, k1 - k0 - 32 * s);
+        advance();
     }
-    // the first stage has landed when at most the loads of the three others are under way
+    // the first stage has landed when at most the loads of the others are under way
     if (steps >= NS) wait_vmcnt63(LPS * (NS - 1));
     else wait_vmcnt63(0);
     wg_barrier_nofence();
@@ -196,6 +206,7 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
     for (int f = 0; f < FM; ++f) fa[0][f] = ra.read(smem, f);
 #pragma unroll
     for (int f = 0; f < FN; ++f) fb[0][f] = rb.read(smem + BM * 64, f);
+    int place = 0;                                                           // of stage t in the ring
     // Stage t: its products, between them the LDS reads of stage t + 1 and the loads of stage t + NS.  FULL: both exist, the latter whole.
     auto stage = [&](auto whole, int t, int u) {
         constexpr bool FULL = decltype(whole)::value;
@@ -204,28 +215,33 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
         else wait_vmcnt63(0);
         __builtin_amdgcn_s_waitcnt(0xC07F);                                  // lgkmcnt(0)
         wg_barrier_nofence();
-        const unsigned char *next = smem + ((t + 1) % NS) * STAGE;            // past the end: what is left in the ring, not used
-        const unsigned to = ring + (t % NS) * STAGE;
+        const unsigned to = ring + place;
+        place = place == (NS - 1) * STAGE ? 0 : place + STAGE;
+        const unsigned char *next = smem + place;                             // past the end: what is left in the ring, not used
         const int kleft = k1 - k0 - 32 * (t + NS);
         const bool more = FULL || t + NS < steps;
+        // One or two other instructions between two pairs of products, which run for as long as those take to issue; none in the last gaps, so that
+        // no LDS read is under way at the end of the stage, where all of them have to have arrived.
 #pragma unroll
-        for (int i = 0; i < FN; ++i) {
+        for (int q = 0; q < GAPS; ++q) {
 #pragma unroll
-            for (int f = i * (FM + FN) / FN; f < (i + 1) * (FM + FN) / FN; ++f) {
-                if (f < FM) fa[u ^ 1][f] = ra.read(next, f);
-                else fb[u ^ 1][f - FM] = rb.read(next + BM * 64, f - FM);
-            }
+            for (int f = 0; f < FM + FN; ++f)
+                if (f * READ_GAPS / (FM + FN) == q) {
+                    if (f < FM) fa[u ^ 1][f] = ra.read(next, f);
+                    else fb[u ^ 1][f - FM] = rb.read(next + BM * 64, f - FM);
+                }
             if (more)
 #pragma unroll
-                for (int f = i * LPS / FN; f < (i + 1) * LPS / FN; ++f) {
-                    if (f < LA) la.template load<FULL>(f, to, wave, kleft);
-                    else lb.template load<FULL>(f - LA, to + BM * 64, wave, kleft);
-                }
-            mm_row(acc[i], fb[u][i], fa[u]);
+                for (int f = 0; f < LPS; ++f)
+                    if (f * READ_GAPS / LPS == q) {
+                        if (f < LA) la.template load<FULL || LIMBS>(f, to, wave, kleft);
+                        else lb.template load<FULL || LIMBS>(f - LA, to + BM * 64, wave, kleft);
+                    }
+            const int i = q / (FM / 2), j = q % (FM / 2) * 2;
+            mm_pair(acc[i][j], acc[i][j + 1], fb[u][i], fa[u][j], fa[u][j + 1]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        la.next();
-        lb.next();
+        advance();
     };
     int s = 0;
     for (; s + NS + 1 < full; s += 2) {
