@@ -59,10 +59,10 @@ struct XentMm {
     int add;                             // SLAB: onto what is there
 };
 
-template <typename T, int BM, int BN, int WM, int WN, bool AT, bool BT, XentEpilogue E>
-__global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
+template <typename T, int BM, int BN, bool AT, bool BT, XentEpilogue E>
+__global__ __launch_bounds__(64 * MM_WAVES) void xent_mm(const XentMm p)
 {
-    constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int FM = BM / 32, FN = BN / 32;
     constexpr bool LIMBS = sizeof(T) == 4;
     extern __shared__ __align__(16) unsigned char smem[];
     const int tiles = p.mm.mt * p.mm.nt, split = blockIdx.x / tiles;
@@ -70,18 +70,17 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
     mm_tile_of(blockIdx.x - split * tiles, tiles, p.mm.mt, p.mm.nt, tm, tn);
     const int k0 = split * p.mm.kper, k1 = p.mm.K - k0 < p.mm.kper ? p.mm.K : k0 + p.mm.kper;
     mm_f32x4 acc[FN][FM];
-    mm_tile<BM, BN, WM, WN, AT, BT, LIMBS>(p.mm, smem, tm * BM, tn * BN, k0, k1, acc);
+    mm_tile<BM, BN, AT, BT, LIMBS ? 3 : 1>(p.mm, smem, tm * BM, tn * BN, k0, k1, acc);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const int wm = (wave % WM) * (BM / WM), wn = (wave / WM) * (BN / WN);
+    const int wm = (wave % 2) * (BM / 2), wn = (wave / 2) * (BN / 2);
     const int m_ = tm * BM + wm + (lane & 15), n_ = tn * BN + wn + 4 * g;       // + 16 fm, + 16 fn + element
     if constexpr (E == XE_STATS) {
-        // a row of the tile: its maximum and sum of exponentials over 4 FN values of a lane, 4 lanes, WN waves
-        float2 *red = reinterpret_cast<float2 *>(smem);                          // [WN][BM]
+        // a row of the tile: its maximum and sum of exponentials over 4 FN values of a lane, 4 lanes, 2 waves
+        float2 *red = reinterpret_cast<float2 *>(smem);                          // [2][BM]
         auto rows = [&](auto whole) {                                            // whole: no columns past the end, which count nothing
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                const int m = m_ + 16 * j;
                 float top = -INFINITY, s = 0.f;
 #pragma unroll
                 for (int i = 0; i < FN; ++i)
@@ -99,7 +98,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
                     }
                 s += __shfl_xor(s, 16, 64);
                 s += __shfl_xor(s, 32, 64);
-                if (g == 0) red[(wave / WM) * BM + wm + 16 * j + lane] = make_float2(top, s);
+                if (g == 0) red[(wave / 2) * BM + wm + 16 * j + lane] = make_float2(top, s);
             }
         };
         if ((tn + 1) * BN <= p.mm.N) rows(std::true_type());
@@ -108,7 +107,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
         for (int j = 0; j < FM; ++j) {
             const int m = m_ + 16 * j;
             const int64_t label = m < p.mm.M ? p.labels[m] - p.v0 : -1;
-            if (label >= tn * BN + wn && label < tn * BN + wn + BN / WN && label < p.mm.N) {
+            if (label >= tn * BN + wn && label < tn * BN + wn + BN / 2 && label < p.mm.N) {
 #pragma unroll
                 for (int i = 0; i < FN; ++i)
 #pragma unroll
@@ -117,14 +116,11 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
             }
         }
         __syncthreads();
-        for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
+        for (int r = threadIdx.x; r < BM; r += 64 * MM_WAVES) {
             float2 v = red[r];
-#pragma unroll
-            for (int w = 1; w < WN; ++w) {
-                const float2 o = red[w * BM + r];
-                const float top = fmaxf(v.x, o.x);                               // the first wave always has columns
-                v = make_float2(top, v.y * __builtin_amdgcn_exp2f(v.x - top) + o.y * __builtin_amdgcn_exp2f(o.x - top));
-            }
+            const float2 o = red[BM + r];
+            const float top = fmaxf(v.x, o.x);                                   // the first wave always has columns
+            v = make_float2(top, v.y * __builtin_amdgcn_exp2f(v.x - top) + o.y * __builtin_amdgcn_exp2f(o.x - top));
             if (tm * BM + r < p.mm.M) p.part[(size_t)tn * p.mm.M + tm * BM + r] = v;
         }
         return;
@@ -156,7 +152,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_mm(const XentMm p)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -row.lse2)) * row.factor;
             const int label = row.label - p.v0;                                  // few waves hold one
-            if (__any(label >= tn * BN + wn && label < tn * BN + wn + BN / WN)) {
+            if (__any(label >= tn * BN + wn && label < tn * BN + wn + BN / 2)) {
 #pragma unroll
                 for (int i = 0; i < FN; ++i)
 #pragma unroll
@@ -291,23 +287,52 @@ __global__ __launch_bounds__(256) void xent_sum(const float *__restrict__ slab, 
     }
 }
 
+// Tile of a product (its edge), and parts of its reduction
+struct MmChoice {
+    int edge, splits;
+};
+
+// Expected time of a product, us, from the tiles of the fullest compute unit: a start and an end per tile and a time per stage of 32.  Two
+// workgroups of a 128 tile and four of a 64 tile share a compute unit and hide each other's waits (three limbs: one and two).
+static float mm_expected(int edge, int limbs, int64_t m, int64_t n, int64_t stages, int splits)
+{
+    const int64_t tiles = ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * splits, per_cu = (tiles + 255) / 256;
+    const float s = (float)((stages + splits - 1) / splits), t = (float)per_cu;
+    if (limbs == 3) return edge == 128 ? t * (5.f + 1.1f * s) : per_cu == 1 ? 3.f + 0.5f * s : t * (1.f + 0.38f * s);
+    if (edge == 256) return t * (10.f + 0.85f * s);
+    if (edge == 128) return (float)(per_cu / 2) * (3.2f + 0.6f * s) + (float)(per_cu % 2) * (2.5f + 0.39f * s);
+    return per_cu == 1 ? 2.f + 0.2f * s : t * (0.6f + 0.125f * s);
+}
+
+static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int limbs, bool split)
+{
+    static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    const int64_t stages = (k + 31) / 32;
+    MmChoice best = {64, 1};
+    float least = INFINITY;
+    const char *forced = env_switch(SW_XENT_TILE);
+    for (int edge = limbs == 3 ? 128 : 256; edge >= 64; edge /= 2)
+        for (int p : parts) {
+            if (p > 1 && (!split || k / p < 256)) break;
+            // parts are written and read again as fp32
+            const float t = mm_expected(edge, limbs, m, n, stages, p) + (p > 1 ? 4.f + (float)m * (float)n * 8.f * (float)p / 4e6f : 0.f);
+            if (t < least && (!forced || atoi(forced) == edge)) {
+                least = t;
+                best = {edge, p};
+            }
+        }
+    return best;
+}
+
 // How a call goes through the vocabulary.  Pieces are as large as 512 MiB of g, and of a copy of w, allow.
 struct XentPlan {
     bool copy;                   // x and w are copied first: fp32, or rows of no multiple of 16 bytes (tensors off that grid are as well)
     int limbs, pitch, piece;     // limbs of an element; elements of a row of x and w as the products read them; classes of a piece
     int64_t krows;               // rows as the products count them where they are the reduction
-    int dx_splits, dw_splits;
+    MmChoice z, dx, dw;          // products of a whole piece
     size_t info, scale, xcopy, wcopy, g, dx_slab, dw_slab, total;        // offsets in the workspace
 };
 
-static int splits_for(int64_t tiles, int64_t k)
-{
-    // parts of at least 512: fewer than half the compute units have a tile otherwise
-    int s = 1;
-    while (tiles * s * 2 <= 256 && k / (s * 2) >= 512) s *= 2;
-    return s;
-}
-static int64_t tiles128(int64_t m, int64_t n) { return ((m + 127) / 128) * ((n + 127) / 128); }
 static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
 
 static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bwd)
@@ -323,8 +348,12 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
     if (piece > most / p.pitch) piece = most / p.pitch;
     p.piece = (int)(piece >= vocab ? vocab : piece < 256 ? 256 : piece / 256 * 256);
     if (p.piece > vocab) p.piece = vocab;
-    p.dx_splits = splits_for(tiles128(rows, width), p.piece);
-    p.dw_splits = splits_for(tiles128(p.piece, width), rows);
+    // only copies and gradients make pieces of the vocabulary (copies are also made of tensors off the 16-byte grid)
+    p.z = mm_choose(rows, p.piece, p.pitch, p.limbs, false);
+    if (bwd) {
+        p.dx = mm_choose(rows, p.pitch, p.piece, p.limbs, true);
+        p.dw = mm_choose(p.piece, p.pitch, rows, p.limbs, true);
+    }
     size_t at = 0;
     auto take = [&](size_t &where, size_t bytes) { where = at; at += r256(bytes); };
     if (!bwd) {
@@ -334,8 +363,8 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         take(p.info, (size_t)rows * sizeof(XentRow));
         take(p.scale, 4);
         take(p.g, (size_t)p.krows * up(p.piece, 64) * 2 * p.limbs);
-        take(p.dx_slab, (size_t)rows * p.pitch * 4 * p.dx_splits);
-        take(p.dw_slab, p.dw_splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw_splits : 0);
+        take(p.dx_slab, (size_t)rows * p.pitch * 4 * p.dx.splits);
+        take(p.dw_slab, p.dw.splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw.splits : 0);
     }
     take(p.xcopy, (size_t)p.krows * p.pitch * 2 * p.limbs);
     take(p.wcopy, (size_t)up(p.piece, 32) * p.pitch * 2 * p.limbs);
@@ -343,34 +372,26 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
     return p;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool AT, bool BT, XentEpilogue E>
+template <typename T, int EDGE, bool AT, bool BT, XentEpilogue E>
 static hipError_t launch_mm_tile(XentMm p, hipStream_t st)
 {
     static LdsLimitOnce lds;
-    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<T, BM, BN, WM, WN, AT, BT, E>));
+    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<T, EDGE, EDGE, AT, BT, E>));
     if (e != hipSuccess) return e;
-    p.mm.mt = (p.mm.M + BM - 1) / BM;
-    p.mm.nt = (p.mm.N + BN - 1) / BN;
+    p.mm.mt = (p.mm.M + EDGE - 1) / EDGE;
+    p.mm.nt = (p.mm.N + EDGE - 1) / EDGE;
     p.mm.kper = (int)up((p.mm.K + p.mm.splits - 1) / p.mm.splits, 32);
-    NGC_LAUNCH((xent_mm<T, BM, BN, WM, WN, AT, BT, E>), dim3((unsigned)(p.mm.mt * p.mm.nt * p.mm.splits)), dim3(64 * WM * WN), (mm_lds_bytes<BM, BN>()), st, p);
+    NGC_LAUNCH((xent_mm<T, EDGE, EDGE, AT, BT, E>), dim3((unsigned)(p.mm.mt * p.mm.nt * p.mm.splits)), dim3(64 * MM_WAVES),
+               (mm_lds_bytes<EDGE, EDGE, sizeof(T) == 4 ? 3 : 1>()), st, p);
     return launch_result();
 }
 
-// The largest tile that still gives most compute units one
-static int mm_tile_size(int64_t m, int64_t n, int splits)
-{
-    if (const char *v = env_switch(SW_XENT_TILE)) return atoi(v);
-    if (((m + 255) / 256) * ((n + 255) / 256) * splits >= 192) return 256;
-    if (tiles128(m, n) * splits >= 128) return 128;
-    return 64;
-}
-
 template <typename T, bool AT, bool BT, XentEpilogue E>
-static hipError_t launch_mm(const XentMm &p, int tile, hipStream_t st)
+static hipError_t launch_mm(const XentMm &p, int edge, hipStream_t st)
 {
-    if (tile == 256) return launch_mm_tile<T, 256, 256, 2, 2, AT, BT, E>(p, st);
-    if (tile == 128) return launch_mm_tile<T, 128, 128, 2, 2, AT, BT, E>(p, st);
-    return launch_mm_tile<T, 64, 64, 2, 2, AT, BT, E>(p, st);
+    if constexpr (sizeof(T) == 2)
+        if (edge == 256) return launch_mm_tile<T, 256, AT, BT, E>(p, st);
+    return edge == 128 ? launch_mm_tile<T, 128, AT, BT, E>(p, st) : launch_mm_tile<T, 64, AT, BT, E>(p, st);
 }
 
 // x or rows of w as the products read them: where they are, or a copy.  all: rows of the copy
@@ -407,9 +428,9 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
         p.mm.blimb = (int64_t)p.mm.N * pl.pitch;
         p.v0 = (int)v0;
         p.part = part + (size_t)tiles * rows;
-        const int tile = mm_tile_size(rows, p.mm.N, 1);
-        if ((e = launch_mm<T, false, false, XE_STATS>(p, tile, st)) != hipSuccess) return e;
-        tiles += (p.mm.N + tile - 1) / tile;
+        const int edge = copy_w ? pl.z.edge : mm_choose(rows, vocab, pl.pitch, pl.limbs, false).edge;
+        if ((e = launch_mm<T, false, false, XE_STATS>(p, edge, st)) != hipSuccess) return e;
+        tiles += (p.mm.N + edge - 1) / edge;
     }
     NGC_LAUNCH(xent_join, dim3((rows + 31) / 32), dim3(256), 0, st, part, p.target, labels, loss, lse, rows, vocab, tiles);
     return launch_result();
@@ -435,7 +456,7 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
     if ((e = launch_result()) != hipSuccess) return e;
     const uint16_t *xp, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
     if ((e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
-    const bool one = pl.piece >= vocab && pl.dx_splits == 1;             // dx leaves the products whole
+    const bool one = pl.piece >= vocab && pl.dx.splits == 1;             // dx leaves the products whole
     for (int64_t v0 = 0; v0 < vocab; v0 += pl.piece) {
         const int piece = vocab - v0 < pl.piece ? (int)(vocab - v0) : pl.piece, gp = (int)up(piece, 64);
         const int kpiece = (int)(pl.limbs == 3 ? up(piece, 32) : piece);
@@ -447,19 +468,18 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
         p.mm.alimb = pl.krows * pl.pitch; p.mm.blimb = (int64_t)kpiece * pl.pitch;
         p.mm.M = rows; p.mm.N = piece; p.mm.K = pl.pitch; p.mm.splits = 1;
         p.out = ws + pl.g; p.ldo = gp; p.glimb = pl.krows * gp; p.store_m = (int)pl.krows; p.store_n = gp;
-        if ((e = launch_mm<T, false, false, XE_GRAD>(p, mm_tile_size(rows, piece, 1), st)) != hipSuccess) return e;
+        if ((e = launch_mm<T, false, false, XE_GRAD>(p, pl.z.edge, st)) != hipSuccess) return e;
         if (dx) {
             XentMm q = p;
             q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
-            q.mm.M = rows; q.mm.N = pl.pitch; q.mm.K = kpiece; q.mm.splits = pl.dx_splits;
+            q.mm.M = rows; q.mm.N = pl.pitch; q.mm.K = kpiece; q.mm.splits = pl.dx.splits;
             q.store_m = rows;
-            const int tile = mm_tile_size(rows, width, pl.dx_splits);
             if (one) {
                 q.out = dx; q.ldo = width; q.store_n = width;
-                e = launch_mm<T, false, true, XE_OUT>(q, tile, st);
+                e = launch_mm<T, false, true, XE_OUT>(q, pl.dx.edge, st);
             } else {
                 q.slab = dx_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = v0 > 0;
-                e = launch_mm<T, false, true, XE_SLAB>(q, tile, st);
+                e = launch_mm<T, false, true, XE_SLAB>(q, pl.dx.edge, st);
             }
             if (e != hipSuccess) return e;
         }
@@ -467,22 +487,21 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             XentMm q = p;
             q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
             q.mm.b = xp; q.mm.blimb = pl.krows * pl.pitch;
-            q.mm.M = piece; q.mm.N = pl.pitch; q.mm.K = (int)pl.krows; q.mm.splits = pl.dw_splits;
+            q.mm.M = piece; q.mm.N = pl.pitch; q.mm.K = (int)pl.krows; q.mm.splits = pl.dw.splits;
             q.store_m = piece;
-            const int tile = mm_tile_size(piece, width, pl.dw_splits);
             T *out = dw + (size_t)v0 * width;
-            if (pl.dw_splits == 1) {
+            if (pl.dw.splits == 1) {
                 q.out = out; q.ldo = width; q.store_n = width;
-                e = launch_mm<T, true, true, XE_OUT>(q, tile, st);
+                e = launch_mm<T, true, true, XE_OUT>(q, pl.dw.edge, st);
             } else {
                 q.slab = dw_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = 0;
-                e = launch_mm<T, true, true, XE_SLAB>(q, tile, st);
-                if (e == hipSuccess) e = sum_slabs(dw_slab, scale, out, piece, width, pl.pitch, pl.dw_splits, st);
+                e = launch_mm<T, true, true, XE_SLAB>(q, pl.dw.edge, st);
+                if (e == hipSuccess) e = sum_slabs(dw_slab, scale, out, piece, width, pl.pitch, pl.dw.splits, st);
             }
             if (e != hipSuccess) return e;
         }
     }
-    return dx && !one ? sum_slabs(dx_slab, scale, dx, rows, width, pl.pitch, pl.dx_splits, st) : hipSuccess;
+    return dx && !one ? sum_slabs(dx_slab, scale, dx, rows, width, pl.pitch, pl.dx.splits, st) : hipSuccess;
 }
 
 size_t linear_xent_workspace(int dtype, int64_t rows, int width, int vocab, bool bwd) { return xent_plan(dtype, rows, width, vocab, bwd).total; }

@@ -2,10 +2,14 @@
 //
 //   c[m][n] = sum_k A(m, k) B(n, k)      A stored [M][K] or (AT) [K][M], B stored [N][K] or (BT) [K][N]
 //
-// A workgroup of WM x WN waves forms a BM x BN tile; a wave BM/WM x BN/WN of it from v_mfma_f32_16x16x32_bf16, whose first operand is B:
-// an accumulator then holds four neighbouring n of one m.  The reduction runs in stages of 32 through a ring of NS stages in LDS, filled by
-// direct global->LDS loads (16 bytes a lane, the scalar base moves along k).  While the products of a stage run, its successor goes from LDS
-// to registers and the stage NS ahead is asked for: one barrier and one counted wait per stage.
+// A workgroup of four waves forms a BM x BN tile; a wave BM/2 x BN/2 of it from v_mfma_f32_16x16x32_bf16, whose first operand is B: an
+// accumulator then holds four neighbouring n of one m.  The reduction runs in stages of 32 through a ring of NS stages in LDS, filled by direct
+// global->LDS loads (16 bytes a lane, the scalar base moves along k).  While the products of a stage run, its successor goes from LDS to
+// registers and the stage NS ahead is asked for: one barrier and one counted wait per stage.
+//
+// L = 3: fp32 operands as sums of three bf16 limbs of 8 significant bits each.  Of the nine products of limbs the six that reach 2^-24 of the
+// result are formed.  A stage holds all limbs, so that a 128 x 128 tile has 96 matrix instructions a wave for its 48 KB where a bf16 one has 16
+// for 16 KB.
 //
 // LDS of a stage, in units of 16 bytes so that 64 lanes fill 1 KB in lane order:
 //   [R][K] operands   rows of 64 bytes; chunk c of row r sits at c ^ (0 or 3 for r / 8 % 2 = 0 or 1).  ds_read_b128 takes lanes 0-3, 12-15, 20-23
@@ -37,18 +41,14 @@ struct MmParams {
     // there has to be zero, and a [K][.] operand has to hold something behind M or N.
     int M, N, K;
     int mt, nt, splits, kper;    // tiles; parts of the reduction and their length (a multiple of 32)
-    int64_t alimb, blimb;        // LIMBS: elements between the limbs of an operand; K is a multiple of 32 then
+    int64_t alimb, blimb;        // L = 3: elements between the limbs of an operand
 };
 
-// LIMBS: fp32 operands as sums of three bf16 limbs, 8 significant bits each.  Of the nine products of limbs the six that reach 2^-24 of the
-// result are formed, one after the other along the reduction: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0).
-constexpr int MM_PAIRS = 6;
-__device__ __forceinline__ int mm_limb_a(int pair) { return pair == 5 ? 2 : (pair >> 1) & ~(pair >> 2) & 1; }
-__device__ __forceinline__ int mm_limb_b(int pair) { return pair == 4 ? 2 : pair & 1 & ~(pair >> 2); }
+constexpr int MM_WAVES = 4;
 
-template <int R, bool T, int NW>
+template <int R, bool T>
 struct MmOperand {
-    static constexpr int LOADS = R / 16 / NW;                            // 1 KB loads per wave and stage
+    static constexpr int NW = MM_WAVES, LOADS = R / 16 / NW;             // 1 KB loads per wave, stage and limb
     static_assert(R % 64 == 0 && LOADS >= 1, "tile");
     uint64_t base;                                                       // of the tile's first row / column, first k of the part
     uint64_t step;                                                       // bytes per stage
@@ -77,18 +77,19 @@ struct MmOperand {
             voff[i] = r0 + r < extent ? 2u * (unsigned)(T ? k * (int)ld + r : r * (int)ld + k) : MM_OOB;
         }
     }
-    // Load i of the stage.  kleft: k that are left from this stage on; FULL: at least 32.  The load goes straight to LDS and has no result
+    // Load i of limb l (`limb` elements from limb to limb) of the stage.  kleft: k that are left from this stage on; FULL: at least 32.  The load goes straight to LDS and has no result
     // register.  It is written out because the compiler waits for every such load that it knows of in front of a transposing LDS read, whatever
     // part of the ring that reads; the waits that are needed are those of mm_tile.
     template <bool FULL>
-    __device__ __forceinline__ void load(int i, unsigned lds, int wave, int kleft) const
+    __device__ __forceinline__ void load(int i, int l, int64_t limb, unsigned lds, int wave, int kleft) const
     {
         typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-        const u32x4 rs = {(unsigned)base, (unsigned)(base >> 32) & 0xFFFFu, 0x7fffffffu, 0x00020000u};
+        const uint64_t at = base + 2 * l * limb;
+        const u32x4 rs = {(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, 0x7fffffffu, 0x00020000u};
         const unsigned v = FULL || kin(i, wave) < kleft ? voff[i] : MM_OOB;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + (unsigned)(i * NW + wave) * 1024u), "v"(v), "s"(rs));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + (unsigned)((l * LOADS + i) * NW + wave) * 1024u), "v"(v), "s"(rs));
     }
-    __device__ __forceinline__ void next(int64_t more) { base += step + more; }
+    __device__ __forceinline__ void next() { base += step; }
 };
 
 // this lane's part of the operand of 16 rows / columns: k 8 (lane / 16) .. + 7
@@ -121,8 +122,9 @@ struct MmFragments {
     }
 };
 
-constexpr int MM_STAGES = 5;
-template <int BM, int BN> constexpr int mm_lds_bytes() { return MM_STAGES * (BM + BN) * 64; }
+// 160 KB of a 256 x 256 tile, two workgroups of a 128 x 128 tile; with three limbs 144 KB of one, two of a 64 x 64 tile
+template <int L> constexpr int mm_stages() { return L == 1 ? 5 : 3; }
+template <int BM, int BN, int L> constexpr int mm_lds_bytes() { return mm_stages<L>() * L * (BM + BN) * 64; }
 
 // Two products, c0 += b a0^T and c1 += b a1^T.  Written out so that the accumulators stay where they are: 256 of them fill the accumulation
 // registers, and the compiler moves them about instead of updating them in place.  The leading wait is the one a matrix instruction needs behind
@@ -153,59 +155,51 @@ __device__ __forceinline__ void mm_tile_of(int id, int total, int mt, int nt, in
 }
 
 // acc[fn][fm]: n = 16 fn + 4 (lane / 16) + element, m = 16 fm + lane % 16 of the wave's part
-template <int BM, int BN, int WM, int WN, bool AT, bool BT, bool LIMBS>
-__device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, int m0, int n0, int k0, int k1, mm_f32x4 (&acc)[BN / WN / 16][BM / WM / 16])
+template <int BM, int BN, bool AT, bool BT, int L>
+__device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, int m0, int n0, int k0, int k1, mm_f32x4 (&acc)[BN / 32][BM / 32])
 {
-    constexpr int NW = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, STAGE = (BM + BN) * 64, NS = MM_STAGES;
-    constexpr int LPS = MmOperand<BM, AT, NW>::LOADS + MmOperand<BN, BT, NW>::LOADS;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    MmOperand<BM, AT, NW> la;
-    MmOperand<BN, BT, NW> lb;
+    constexpr int FM = BM / 32, FN = BN / 32, STAGE = L * (BM + BN) * 64, NS = mm_stages<L>();
+    constexpr int LA = MmOperand<BM, AT>::LOADS * L, LB = MmOperand<BN, BT>::LOADS * L, LPS = LA + LB;
+    static_assert(L == 1 || L == 3, "limbs");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    MmOperand<BM, AT> la;
+    MmOperand<BN, BT> lb;
     la.init(p.a, p.lda, m0, p.M, k0, wave);
     lb.init(p.b, p.ldb, n0, p.N, k0, wave);
     MmFragments<BM, AT> ra;
     MmFragments<BN, BT> rb;
-    ra.init((wave % WM) * (BM / WM), lane);
-    rb.init((wave / WM) * (BN / WN), lane);
-    const int per = (k1 - k0 + 31) / 32, steps = LIMBS ? MM_PAIRS * per : per, full = LIMBS ? steps : (k1 - k0) / 32;
-    int asked = 0, pair = 0;                                                 // LIMBS: stages of this pair that were asked for
-    auto advance = [&] {
-        int64_t more_a = 0, more_b = 0;
-        if constexpr (LIMBS) {
-            const bool wrap = ++asked == per;
-            const int64_t ja = 2 * (mm_limb_a(pair + 1) - mm_limb_a(pair)) * p.alimb - (int64_t)per * la.step;
-            const int64_t jb = 2 * (mm_limb_b(pair + 1) - mm_limb_b(pair)) * p.blimb - (int64_t)per * lb.step;
-            more_a = wrap ? ja : 0;
-            more_b = wrap ? jb : 0;
-            pair += wrap ? 1 : 0;
-            asked = wrap ? 0 : asked;
-        }
-        la.next(more_a);
-        lb.next(more_b);
-    };
+    ra.init((wave % 2) * (BM / 2), lane);
+    rb.init((wave / 2) * (BN / 2), lane);
+    const int steps = (k1 - k0 + 31) / 32, full = (k1 - k0) / 32;
     const unsigned ring = (unsigned)(uintptr_t)(mm_lds_void *)smem;          // LDS address
-    constexpr int LA = MmOperand<BM, AT, NW>::LOADS, LB = MmOperand<BN, BT, NW>::LOADS;
-    constexpr int GAPS = FN * FM / 2, READ_GAPS = GAPS * 3 / 4 > 0 ? GAPS * 3 / 4 : 1;
-    mm_bf16x8 fa[2][FM], fb[2][FN];
+    auto load = [&](auto whole, int f, unsigned to, int kleft) {             // load f of a stage
+        constexpr bool FULL = decltype(whole)::value;
+        if (f < LA) la.template load<FULL>(f % (LA / L), f / (LA / L), p.alimb, to, wave, kleft);
+        else lb.template load<FULL>((f - LA) % (LB / L), (f - LA) / (LB / L), p.blimb, to + L * BM * 64, wave, kleft);
+    };
+    // the PAIRS products of limbs, and the GAPS between pairs of matrix instructions of a stage
+    constexpr int PAIRS = L == 3 ? 6 : 1, GAPS = PAIRS * FN * FM / 2, READS = L * (FM + FN), ITEM_GAPS = GAPS * 3 / 4 > 0 ? GAPS * 3 / 4 : 1;
+    mm_bf16x8 fa[2][L][FM], fb[2][L][FN];
+    auto read = [&](int f, const unsigned char *st, int u) {                 // fragment f of a stage
+        if (f < L * FM) fa[u][f / FM][f % FM] = ra.read(st + f / FM * BM * 64, f % FM);
+        else fb[u][(f - L * FM) / FN][(f - L * FM) % FN] = rb.read(st + L * BM * 64 + (f - L * FM) / FN * BN * 64, (f - L * FM) % FN);
+    };
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
         for (int j = 0; j < FM; ++j) acc[i][j] = mm_f32x4{0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < NS && s < steps; ++s) {
 #pragma unroll
-        for (int i = 0; i < LA; ++i) la.template load<LIMBS>(i, ring + s * STAGE, wave, k1 - k0 - 32 * s);
-#pragma unroll
-        for (int i = 0; i < LB; ++i) lb.template load<LIMBS>(i, ring + s * STAGE + BM * 64, wave, k1 - k0 - 32 * s);
-        advance();
+        for (int f = 0; f < LPS; ++f) load(std::false_type(), f, ring + s * STAGE, k1 - k0 - 32 * s);
+        la.next();
+        lb.next();
     }
     // the first stage has landed when at most the loads of the others are under way
     if (steps >= NS) wait_vmcnt63(LPS * (NS - 1));
     else wait_vmcnt63(0);
     wg_barrier_nofence();
 #pragma unroll
-    for (int f = 0; f < FM; ++f) fa[0][f] = ra.read(smem, f);
-#pragma unroll
-    for (int f = 0; f < FN; ++f) fb[0][f] = rb.read(smem + BM * 64, f);
+    for (int f = 0; f < READS; ++f) read(f, smem, 0);
     int place = 0;                                                           // of stage t in the ring
     // Stage t: its products, between them the LDS reads of stage t + 1 and the loads of stage t + NS.  FULL: both exist, the latter whole.
     auto stage = [&](auto whole, int t, int u) {
@@ -225,23 +219,20 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
 #pragma unroll
         for (int q = 0; q < GAPS; ++q) {
 #pragma unroll
-            for (int f = 0; f < FM + FN; ++f)
-                if (f * READ_GAPS / (FM + FN) == q) {
-                    if (f < FM) fa[u ^ 1][f] = ra.read(next, f);
-                    else fb[u ^ 1][f - FM] = rb.read(next + BM * 64, f - FM);
-                }
+            for (int f = 0; f < READS; ++f)
+                if (f * ITEM_GAPS / READS == q) read(f, next, u ^ 1);
             if (more)
 #pragma unroll
                 for (int f = 0; f < LPS; ++f)
-                    if (f * READ_GAPS / LPS == q) {
-                        if (f < LA) la.template load<FULL || LIMBS>(f, to, wave, kleft);
-                        else lb.template load<FULL || LIMBS>(f - LA, to + BM * 64, wave, kleft);
-                    }
-            const int i = q / (FM / 2), j = q % (FM / 2) * 2;
-            mm_pair(acc[i][j], acc[i][j + 1], fb[u][i], fa[u][j], fa[u][j + 1]);
+                    if (f * ITEM_GAPS / LPS == q) load(whole, f, to, kleft);
+            // products of limbs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
+            const int pair = q / (FN * FM / 2), i = q % (FN * FM / 2) / (FM / 2), j = q % (FM / 2) * 2;
+            const int l = pair == 5 ? 2 : pair == 2 || pair == 3 ? 1 : 0, r = pair == 4 ? 2 : pair == 1 || pair == 3 ? 1 : 0;
+            mm_pair(acc[i][j], acc[i][j + 1], fb[u][r][i], fa[u][l][j], fa[u][l][j + 1]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        advance();
+        la.next();
+        lb.next();
     };
     int s = 0;
     for (; s + NS + 1 < full; s += 2) {
