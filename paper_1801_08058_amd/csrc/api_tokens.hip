@@ -28,6 +28,14 @@ bool sizes_ok(int64_t rows, int64_t cols)
 
 constexpr int32_t EMBEDDING_BWD_VOCAB = 1 << 21;
 
+// The operands and the logits of a linear layer: the tiles of their products stay within a grid, and offsets inside a tile below 2 GiB
+bool xent_sizes_ok(int64_t rows, int32_t width, int32_t vocab)
+{
+    constexpr unsigned long long most = 1ull << 37;
+    return sizes_ok(rows, width) && sizes_ok(vocab, width) && width < (1 << 20) && (unsigned long long)rows * (unsigned)width < most &&
+           (unsigned long long)(unsigned)vocab * (unsigned)width < most && (unsigned long long)rows * (unsigned)vocab < most;
+}
+
 }  // namespace
 
 extern "C" {
@@ -87,14 +95,14 @@ int ngc_layer_norm_bwd(int32_t dtype, int64_t rows, int32_t cols, const void *x,
 
 size_t ngc_linear_xent_workspace_bytes(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, int32_t bwd)
 {
-    return known_type(dtype) && sizes_ok(rows, width) && sizes_ok(vocab, width) ? linear_xent_workspace(dtype, rows, width, vocab, bwd != 0) : 0;
+    return known_type(dtype) && xent_sizes_ok(rows, width, vocab) ? linear_xent_workspace(dtype, rows, width, vocab, bwd != 0) : 0;
 }
 
 int ngc_linear_xent(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, const void *x, const void *w, const int64_t *labels, float *loss,
                     float *lse, void *ws, size_t ws_bytes, void *hip_stream)
 {
     if (!known_type(dtype)) return NGC_BAD_ARG;
-    if (!sizes_ok(rows, width) || !sizes_ok(vocab, width)) return NGC_BAD_SHAPE;
+    if (!xent_sizes_ok(rows, width, vocab)) return NGC_BAD_SHAPE;
     if (!x || !w || !labels || !loss || !lse || off(x, elem_mask(dtype)) || off(w, elem_mask(dtype)) || off(labels, 7) || off(loss, 3) || off(lse, 3) ||
         off(ws, 15))
         return NGC_BAD_ARG;
@@ -106,7 +114,7 @@ int ngc_linear_xent_bwd(int32_t dtype, int64_t rows, int32_t width, int32_t voca
                         const float *lse, const float *dloss, void *dx, void *dw, void *ws, size_t ws_bytes, void *hip_stream)
 {
     if (!known_type(dtype)) return NGC_BAD_ARG;
-    if (!sizes_ok(rows, width) || !sizes_ok(vocab, width)) return NGC_BAD_SHAPE;
+    if (!xent_sizes_ok(rows, width, vocab)) return NGC_BAD_SHAPE;
     if (!x || !w || !labels || !lse || !dloss || (!dx && !dw) || off(x, elem_mask(dtype)) || off(w, elem_mask(dtype)) || off(labels, 7) || off(lse, 3) ||
         off(dloss, 3) || off(dx, elem_mask(dtype)) || off(dw, elem_mask(dtype)) || off(ws, 15))
         return NGC_BAD_ARG;

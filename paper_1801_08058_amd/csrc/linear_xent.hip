@@ -60,14 +60,14 @@ struct XentMm {
 };
 
 template <typename T, int BM, int BN, bool AT, bool BT, XentEpilogue E>
-__global__ __launch_bounds__(64 * MM_WAVES) void xent_mm(const XentMm p)
+__device__ __forceinline__ void xent_product(const XentMm &p, int block)
 {
     constexpr int FM = BM / 32, FN = BN / 32;
     constexpr bool LIMBS = sizeof(T) == 4;
     extern __shared__ __align__(16) unsigned char smem[];
-    const int tiles = p.mm.mt * p.mm.nt, split = blockIdx.x / tiles;
+    const int tiles = p.mm.mt * p.mm.nt, split = block / tiles;
     int tm, tn;
-    mm_tile_of(blockIdx.x - split * tiles, tiles, p.mm.mt, p.mm.nt, tm, tn);
+    mm_tile_of(block - split * tiles, tiles, p.mm.mt, p.mm.nt, tm, tn);
     const int k0 = split * p.mm.kper, k1 = p.mm.K - k0 < p.mm.kper ? p.mm.K : k0 + p.mm.kper;
     mm_f32x4 acc[FN][FM];
     mm_tile<BM, BN, AT, BT, LIMBS ? 3 : 1>(p.mm, smem, tm * BM, tn * BN, k0, k1, acc);
@@ -78,6 +78,12 @@ __global__ __launch_bounds__(64 * MM_WAVES) void xent_mm(const XentMm p)
     if constexpr (E == XE_STATS) {
         // a row of the tile: its maximum and sum of exponentials over 4 FN values of a lane, 4 lanes, 2 waves
         float2 *red = reinterpret_cast<float2 *>(smem);                          // [2][BM]
+        int label[FM];                                                           // class of the piece, or -1
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            const int64_t at = m_ + 16 * j < p.mm.M ? p.labels[m_ + 16 * j] - p.v0 : -1;
+            label[j] = at >= 0 && at < p.mm.N ? (int)at : -1;
+        }
         auto rows = [&](auto whole) {                                            // whole: no columns past the end, which count nothing
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
@@ -99,22 +105,17 @@ __global__ __launch_bounds__(64 * MM_WAVES) void xent_mm(const XentMm p)
                 s += __shfl_xor(s, 16, 64);
                 s += __shfl_xor(s, 32, 64);
                 if (g == 0) red[(wave / 2) * BM + wm + 16 * j + lane] = make_float2(top, s);
+                if (label[j] >= tn * BN + wn && label[j] < tn * BN + wn + BN / 2) {      // in the same pass: 256 values are not kept for another
+#pragma unroll
+                    for (int i = 0; i < FN; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (label[j] == n_ + 16 * i + e) p.target[m_ + 16 * j] = acc[i][j][e];
+                }
             }
         };
         if ((tn + 1) * BN <= p.mm.N) rows(std::true_type());
         else rows(std::false_type());
-#pragma unroll
-        for (int j = 0; j < FM; ++j) {
-            const int m = m_ + 16 * j;
-            const int64_t label = m < p.mm.M ? p.labels[m] - p.v0 : -1;
-            if (label >= tn * BN + wn && label < tn * BN + wn + BN / 2 && label < p.mm.N) {
-#pragma unroll
-                for (int i = 0; i < FN; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (label == n_ + 16 * i + e) p.target[m] = acc[i][j][e];
-            }
-        }
         __syncthreads();
         for (int r = threadIdx.x; r < BM; r += 64 * MM_WAVES) {
             float2 v = red[r];
@@ -223,6 +224,90 @@ __global__ __launch_bounds__(64 * MM_WAVES) void xent_mm(const XentMm p)
     }
 }
 
+template <typename T, int EDGE, bool AT, bool BT, XentEpilogue E>
+__global__ __launch_bounds__(64 * MM_WAVES) void xent_mm(const XentMm p)
+{
+    xent_product<T, EDGE, EDGE, AT, BT, E>(p, blockIdx.x);
+}
+
+// dx and dw of one piece, which both read g: the workgroups of dx, then those of dw
+template <typename T, int EDGE, XentEpilogue EDX>
+__global__ __launch_bounds__(64 * MM_WAVES) void xent_mm_both(const XentMm dx, const XentMm dw, int first)
+{
+    if ((int)blockIdx.x < first) xent_product<T, EDGE, EDGE, false, true, EDX>(dx, blockIdx.x);
+    else xent_product<T, EDGE, EDGE, true, true, XE_OUT>(dw, blockIdx.x - first);
+}
+
+// Few tiles: the logits' product runs in parts (fp32 slabs, `stride` elements apart, rows of `ld`), and a workgroup per row adds them up.
+__device__ __forceinline__ mm_f32x4 sum_parts(const float *at, int splits, size_t stride)
+{
+    mm_f32x4 v = *reinterpret_cast<const mm_f32x4 *>(at);
+#pragma unroll 4
+    for (int q = 1; q < splits; ++q) v += *reinterpret_cast<const mm_f32x4 *>(at + q * stride);
+    return v;
+}
+
+__global__ __launch_bounds__(256) void xent_row_loss(const float *__restrict__ slab, int splits, size_t stride, int ld, const int64_t *__restrict__ labels,
+                                                     float *__restrict__ loss, float *__restrict__ lse, int vocab)
+{
+    __shared__ float sm[4], target;
+    const int m = blockIdx.x;
+    const int64_t label = labels[m];
+    const bool live = label >= 0 && label < vocab;
+    float top = -INFINITY, s = 0.f;
+    for (int v = threadIdx.x * 4; v < vocab; v += 1024) {
+        const mm_f32x4 z = sum_parts(slab + (size_t)m * ld + v, splits, stride);
+        float up = top;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (v + e < vocab) {
+                up = fmaxf(up, z[e] * LOG2E);
+                if (label == v + e) target = z[e];
+            }
+        s *= __builtin_amdgcn_exp2f(top - up);                                   // 0 the first time
+        top = up;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += v + e < vocab ? __builtin_amdgcn_exp2f(fmaf(z[e], LOG2E, -top)) : 0.f;
+    }
+    const float all = block_reduce<4>(top, true, sm);
+    s = block_reduce<4>(top == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f(top - all), false, sm);
+    if (threadIdx.x) return;
+    const float l = (all + log2f(s)) * LN2;
+    lse[m] = l;
+    loss[m] = live ? l - target : 0.f;
+}
+
+// g of a row, as xent_rows and the epilogue of the product form it; rows from `rows` on are zeros.  Workgroup 0 leaves the scale.
+template <typename T>
+__global__ __launch_bounds__(256) void xent_row_grad(const float *__restrict__ slab, int splits, size_t stride, int ld, const int64_t *__restrict__ labels,
+                                                     const float *__restrict__ lse, const float *__restrict__ dloss, uint16_t *__restrict__ g,
+                                                     int64_t glimb, int gp, float *__restrict__ scale, int rows, int vocab)
+{
+    __shared__ float sm[4];
+    const int m = blockIdx.x;
+    float most = 0.f;
+    for (int r = threadIdx.x; r < rows; r += 256)
+        if (labels[r] >= 0 && labels[r] < vocab) most = fmaxf(most, fabsf(dloss[r]));
+    most = fmaxf(block_reduce<4>(most, true, sm), 0x1p-100f);
+    if (m == 0 && threadIdx.x == 0) *scale = most;
+    const int64_t label = m < rows ? labels[m] : -1;
+    const bool live = label >= 0 && label < vocab;
+    const float factor = live ? dloss[m] * (1.0f / most) : 0.f, lse2 = live ? lse[m] * LOG2E : 0.f;
+    for (int v = threadIdx.x * 4; v < gp; v += 1024) {
+        mm_f32x4 z = mm_f32x4{0.f, 0.f, 0.f, 0.f};
+        if (live && v < vocab) z = sum_parts(slab + (size_t)m * ld + v, splits, stride);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            z[e] = live && v + e < vocab ? __builtin_amdgcn_exp2f(fmaf(z[e], LOG2E, -lse2)) * factor - (label == v + e ? factor : 0.f) : 0.f;
+#pragma unroll
+        for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
+            const uint2 b = make_uint2(pack_bf16x2_hw(z[0], z[1]), pack_bf16x2_hw(z[2], z[3]));
+            *reinterpret_cast<uint2 *>(g + l * glimb + (size_t)m * gp + v) = b;
+            z -= mm_f32x4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xFFFF0000u), __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xFFFF0000u)};
+        }
+    }
+}
+
 // lse and loss of 32 rows from the tiles' maxima and sums, eight parts of the tiles each
 __global__ __launch_bounds__(256) void xent_join(const float2 *__restrict__ part, const float *__restrict__ target, const int64_t *__restrict__ labels,
                                                   float *__restrict__ loss, float *__restrict__ lse, int rows, int vocab, int tiles)
@@ -287,39 +372,38 @@ __global__ __launch_bounds__(256) void xent_sum(const float *__restrict__ slab, 
     }
 }
 
-// Tile of a product (its edge), and parts of its reduction
+// Tile of a product (its edge), parts of its reduction, and the expected time, us
 struct MmChoice {
     int edge, splits;
+    float us;
 };
 
-// Expected time of a product, us, from the tiles of the fullest compute unit: a start and an end per tile and a time per stage of 32.  Two
-// workgroups of a 128 tile and four of a 64 tile share a compute unit and hide each other's waits (three limbs: one and two).
+// From the tiles of the fullest compute unit: a start and an end per tile and a time per stage of 32.  Two workgroups of a 128 tile and four of a
+// 64 tile share a compute unit and hide each other's waits (three limbs: one and two).
 static float mm_expected(int edge, int limbs, int64_t m, int64_t n, int64_t stages, int splits)
 {
     const int64_t tiles = ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * splits, per_cu = (tiles + 255) / 256;
     const float s = (float)((stages + splits - 1) / splits), t = (float)per_cu;
     if (limbs == 3) return edge == 128 ? t * (5.f + 1.1f * s) : per_cu == 1 ? 3.f + 0.5f * s : t * (1.f + 0.38f * s);
     if (edge == 256) return t * (10.f + 0.85f * s);
-    if (edge == 128) return (float)(per_cu / 2) * (3.2f + 0.6f * s) + (float)(per_cu % 2) * (2.5f + 0.39f * s);
-    return per_cu == 1 ? 2.f + 0.2f * s : t * (0.6f + 0.125f * s);
+    if (edge == 128) return (float)(per_cu / 2) * (3.f + 0.54f * s) + (float)(per_cu % 2) * (2.5f + 0.39f * s);
+    return per_cu == 1 ? 2.f + 0.2f * s : t * (0.6f + 0.115f * s);
 }
 
-static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int limbs, bool split)
+// most: parts at most; slab: also a single part is written and read again as fp32
+static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int limbs, int most, bool slab)
 {
     static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     const int64_t stages = (k + 31) / 32;
-    MmChoice best = {64, 1};
-    float least = INFINITY;
+    // what memory takes for the operands: a small tile is no faster than a large one then
+    const float bytes = ((float)m + (float)n) * (float)k * 2.f * (float)limbs / 4.4e6f;
+    MmChoice best = {64, 1, INFINITY};
     const char *forced = env_switch(SW_XENT_TILE);
-    for (int edge = limbs == 3 ? 128 : 256; edge >= 64; edge /= 2)
+    for (int edge = limbs == 3 || slab ? 128 : 256; edge >= 64; edge /= 2)
         for (int p : parts) {
-            if (p > 1 && (!split || k / p < 256)) break;
-            // parts are written and read again as fp32
-            const float t = mm_expected(edge, limbs, m, n, stages, p) + (p > 1 ? 4.f + (float)m * (float)n * 8.f * (float)p / 4e6f : 0.f);
-            if (t < least && (!forced || atoi(forced) == edge)) {
-                least = t;
-                best = {edge, p};
-            }
+            if (p > most || (p > 1 && k / p < 128)) break;
+            const float run = mm_expected(edge, limbs, m, n, stages, p), t = (run > bytes ? run : bytes) + (p > 1 || slab ? 3.f + (float)m * (float)n * 8.f * (float)p / 4e6f : 0.f);
+            if (t < best.us && (!forced || atoi(forced) == edge || (slab && best.us == INFINITY))) best = {edge, p, t};
         }
     return best;
 }
@@ -330,7 +414,8 @@ struct XentPlan {
     int limbs, pitch, piece;     // limbs of an element; elements of a row of x and w as the products read them; classes of a piece
     int64_t krows;               // rows as the products count them where they are the reduction
     MmChoice z, dx, dw;          // products of a whole piece
-    size_t info, scale, xcopy, wcopy, g, dx_slab, dw_slab, total;        // offsets in the workspace
+    bool by_rows;                // z in slabs, then a workgroup per row
+    size_t info, scale, zslab, xcopy, wcopy, g, dx_slab, dw_slab, total; // offsets in the workspace
 };
 
 static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
@@ -346,16 +431,25 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
     int64_t piece = vocab;
     if (bwd && piece > most / p.krows) piece = most / p.krows;
     if (piece > most / p.pitch) piece = most / p.pitch;
+    if (piece > (1 << 21)) piece = 1 << 21;                              // offsets in a tile of g stay below 2 GiB
     p.piece = (int)(piece >= vocab ? vocab : piece < 256 ? 256 : piece / 256 * 256);
     if (p.piece > vocab) p.piece = vocab;
     // only copies and gradients make pieces of the vocabulary (copies are also made of tensors off the 16-byte grid)
-    p.z = mm_choose(rows, p.piece, p.pitch, p.limbs, false);
+    p.z = mm_choose(rows, p.piece, p.pitch, p.limbs, 1, false);
     if (bwd) {
-        p.dx = mm_choose(rows, p.pitch, p.piece, p.limbs, true);
-        p.dw = mm_choose(p.piece, p.pitch, rows, p.limbs, true);
+        p.dx = mm_choose(rows, p.pitch, p.piece, p.limbs, 64, false);
+        p.dw = mm_choose(p.piece, p.pitch, rows, p.limbs, 64, false);
+    }
+    // One piece of few tiles: in parts, as long as these take no more than 32 MiB and (backprop: every row looks at all weights) the rows are few.
+    // Two launches either way.
+    if (p.piece == vocab && rows <= 1024) {
+        const MmChoice parts = mm_choose(rows, vocab, p.pitch, p.limbs, 64, true);
+        p.by_rows = parts.us < p.z.us && (int64_t)rows * up(vocab, 8) * 4 * parts.splits <= (32 << 20);
+        if (p.by_rows) p.z = parts;
     }
     size_t at = 0;
     auto take = [&](size_t &where, size_t bytes) { where = at; at += r256(bytes); };
+    if (p.by_rows) take(p.zslab, (size_t)rows * up(vocab, 8) * 4 * p.z.splits);
     if (!bwd) {
         take(p.info, (size_t)rows * 8 * ((size_t)((int64_t)vocab + 63) / 64 + (vocab - 1) / p.piece + 1));       // part
         take(p.scale, (size_t)rows * 4);                                                                        // target
@@ -372,16 +466,22 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
     return p;
 }
 
+static unsigned mm_grid(MmParams &mm, int edge)
+{
+    mm.mt = (mm.M + edge - 1) / edge;
+    mm.nt = (mm.N + edge - 1) / edge;
+    mm.kper = (int)up((mm.K + mm.splits - 1) / mm.splits, 32);
+    return (unsigned)(mm.mt * mm.nt * mm.splits);
+}
+
 template <typename T, int EDGE, bool AT, bool BT, XentEpilogue E>
 static hipError_t launch_mm_tile(XentMm p, hipStream_t st)
 {
     static LdsLimitOnce lds;
-    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<T, EDGE, EDGE, AT, BT, E>));
+    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<T, EDGE, AT, BT, E>));
     if (e != hipSuccess) return e;
-    p.mm.mt = (p.mm.M + EDGE - 1) / EDGE;
-    p.mm.nt = (p.mm.N + EDGE - 1) / EDGE;
-    p.mm.kper = (int)up((p.mm.K + p.mm.splits - 1) / p.mm.splits, 32);
-    NGC_LAUNCH((xent_mm<T, EDGE, EDGE, AT, BT, E>), dim3((unsigned)(p.mm.mt * p.mm.nt * p.mm.splits)), dim3(64 * MM_WAVES),
+    const unsigned grid = mm_grid(p.mm, EDGE);
+    NGC_LAUNCH((xent_mm<T, EDGE, AT, BT, E>), dim3(grid), dim3(64 * MM_WAVES),
                (mm_lds_bytes<EDGE, EDGE, sizeof(T) == 4 ? 3 : 1>()), st, p);
     return launch_result();
 }
@@ -389,9 +489,20 @@ static hipError_t launch_mm_tile(XentMm p, hipStream_t st)
 template <typename T, bool AT, bool BT, XentEpilogue E>
 static hipError_t launch_mm(const XentMm &p, int edge, hipStream_t st)
 {
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2 && !(E == XE_SLAB && !BT))                      // slabs of z: 128 at most
         if (edge == 256) return launch_mm_tile<T, 256, AT, BT, E>(p, st);
     return edge == 128 ? launch_mm_tile<T, 128, AT, BT, E>(p, st) : launch_mm_tile<T, 64, AT, BT, E>(p, st);
+}
+
+template <typename T, int EDGE, XentEpilogue EDX>
+static hipError_t launch_both(XentMm dx, XentMm dw, hipStream_t st)
+{
+    static LdsLimitOnce lds;
+    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm_both<T, EDGE, EDX>));
+    if (e != hipSuccess) return e;
+    const unsigned first = mm_grid(dx.mm, EDGE), grid = first + mm_grid(dw.mm, EDGE);
+    NGC_LAUNCH((xent_mm_both<T, EDGE, EDX>), dim3(grid), dim3(64 * MM_WAVES), (mm_lds_bytes<EDGE, EDGE, sizeof(T) == 4 ? 3 : 1>()), st, dx, dw, (int)first);
+    return launch_result();
 }
 
 // x or rows of w as the products read them: where they are, or a copy.  all: rows of the copy
@@ -428,7 +539,16 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
         p.mm.blimb = (int64_t)p.mm.N * pl.pitch;
         p.v0 = (int)v0;
         p.part = part + (size_t)tiles * rows;
-        const int edge = copy_w ? pl.z.edge : mm_choose(rows, vocab, pl.pitch, pl.limbs, false).edge;
+        if (pl.by_rows) {                                                // one piece
+            const int ld = (int)up(vocab, 8);
+            p.slab = reinterpret_cast<float *>(ws + pl.zslab);
+            p.ldo = p.store_n = ld; p.store_m = rows;
+            p.mm.splits = pl.z.splits;
+            if ((e = launch_mm<T, false, false, XE_SLAB>(p, pl.z.edge, st)) != hipSuccess) return e;
+            NGC_LAUNCH(xent_row_loss, dim3(rows), dim3(256), 0, st, p.slab, pl.z.splits, (size_t)rows * ld, ld, labels, loss, lse, vocab);
+            return launch_result();
+        }
+        const int edge = copy_w || pl.piece == vocab ? pl.z.edge : mm_choose(rows, vocab, pl.pitch, pl.limbs, 1, false).edge;
         if ((e = launch_mm<T, false, false, XE_STATS>(p, edge, st)) != hipSuccess) return e;
         tiles += (p.mm.N + edge - 1) / edge;
     }
@@ -451,12 +571,13 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
     const XentPlan pl = xent_plan(sizeof(T) == 4 ? NGC_F32 : NGC_BF16, rows, width, vocab, true);
     XentRow *info = reinterpret_cast<XentRow *>(ws + pl.info);
     float *scale = reinterpret_cast<float *>(ws + pl.scale), *dx_slab = reinterpret_cast<float *>(ws + pl.dx_slab), *dw_slab = reinterpret_cast<float *>(ws + pl.dw_slab);
-    hipError_t e;
-    NGC_LAUNCH(xent_rows, dim3(1), dim3(1024), 0, st, labels, lse, dloss, info, scale, rows, vocab);
-    if ((e = launch_result()) != hipSuccess) return e;
+    hipError_t e = hipSuccess;
+    if (!pl.by_rows) NGC_LAUNCH(xent_rows, dim3(1), dim3(1024), 0, st, labels, lse, dloss, info, scale, rows, vocab);
+    if (!pl.by_rows && (e = launch_result()) != hipSuccess) return e;
     const uint16_t *xp, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
     if ((e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
     const bool one = pl.piece >= vocab && pl.dx.splits == 1;             // dx leaves the products whole
+    const bool together = dx && dw && pl.dw.splits == 1 && pl.dx.edge == pl.dw.edge && pl.dw.edge < 256;
     for (int64_t v0 = 0; v0 < vocab; v0 += pl.piece) {
         const int piece = vocab - v0 < pl.piece ? (int)(vocab - v0) : pl.piece, gp = (int)up(piece, 64);
         const int kpiece = (int)(pl.limbs == 3 ? up(piece, 32) : piece);
@@ -468,7 +589,21 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
         p.mm.alimb = pl.krows * pl.pitch; p.mm.blimb = (int64_t)kpiece * pl.pitch;
         p.mm.M = rows; p.mm.N = piece; p.mm.K = pl.pitch; p.mm.splits = 1;
         p.out = ws + pl.g; p.ldo = gp; p.glimb = pl.krows * gp; p.store_m = (int)pl.krows; p.store_n = gp;
-        if ((e = launch_mm<T, false, false, XE_GRAD>(p, pl.z.edge, st)) != hipSuccess) return e;
+        if (pl.by_rows) {                                                // one piece
+            const int ld = (int)up(vocab, 8);
+            XentMm q = p;
+            q.slab = reinterpret_cast<float *>(ws + pl.zslab);
+            q.ldo = q.store_n = ld; q.store_m = rows;
+            q.mm.splits = pl.z.splits;
+            if ((e = launch_mm<T, false, false, XE_SLAB>(q, pl.z.edge, st)) != hipSuccess) return e;
+            NGC_LAUNCH((xent_row_grad<T>), dim3((unsigned)pl.krows), dim3(256), 0, st, q.slab, pl.z.splits, (size_t)rows * ld, ld, labels, lse, dloss,
+                       reinterpret_cast<uint16_t *>(ws + pl.g), p.glimb, gp, scale, rows, vocab);
+            e = launch_result();
+        } else {
+            e = launch_mm<T, false, false, XE_GRAD>(p, pl.z.edge, st);
+        }
+        if (e != hipSuccess) return e;
+        XentMm both{};                                                   // dx, while it waits to run together with dw
         if (dx) {
             XentMm q = p;
             q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
@@ -476,12 +611,13 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             q.store_m = rows;
             if (one) {
                 q.out = dx; q.ldo = width; q.store_n = width;
-                e = launch_mm<T, false, true, XE_OUT>(q, pl.dx.edge, st);
+                if (!together) e = launch_mm<T, false, true, XE_OUT>(q, pl.dx.edge, st);
             } else {
                 q.slab = dx_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = v0 > 0;
-                e = launch_mm<T, false, true, XE_SLAB>(q, pl.dx.edge, st);
+                if (!together) e = launch_mm<T, false, true, XE_SLAB>(q, pl.dx.edge, st);
             }
             if (e != hipSuccess) return e;
+            both = q;
         }
         if (dw) {
             XentMm q = p;
@@ -492,7 +628,9 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             T *out = dw + (size_t)v0 * width;
             if (pl.dw.splits == 1) {
                 q.out = out; q.ldo = width; q.store_n = width;
-                e = launch_mm<T, true, true, XE_OUT>(q, pl.dw.edge, st);
+                if (!together) e = launch_mm<T, true, true, XE_OUT>(q, pl.dw.edge, st);
+                else if (pl.dw.edge == 128) e = one ? launch_both<T, 128, XE_OUT>(both, q, st) : launch_both<T, 128, XE_SLAB>(both, q, st);
+                else e = one ? launch_both<T, 64, XE_OUT>(both, q, st) : launch_both<T, 64, XE_SLAB>(both, q, st);
             } else {
                 q.slab = dw_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = 0;
                 e = launch_mm<T, true, true, XE_SLAB>(q, pl.dw.edge, st);
