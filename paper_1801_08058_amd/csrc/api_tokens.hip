@@ -32,7 +32,7 @@ constexpr int32_t EMBEDDING_BWD_VOCAB = 1 << 21;
 bool xent_sizes_ok(int64_t rows, int32_t width, int32_t vocab)
 {
     constexpr unsigned long long most = 1ull << 37;
-    return sizes_ok(rows, width) && sizes_ok(vocab, width) && width < (1 << 20) && (unsigned long long)rows * (unsigned)width < most &&
+    return sizes_ok(rows, width) && sizes_ok(vocab, width) && rows < (1 << 28) && vocab < (1 << 28) && width < (1 << 20) && (unsigned long long)rows * (unsigned)width < most &&
            (unsigned long long)(unsigned)vocab * (unsigned)width < most && (unsigned long long)rows * (unsigned)vocab < most;
 }
 

@@ -238,7 +238,8 @@ __global__ __launch_bounds__(1024) void layer_norm_long(const T *x, const float 
     constexpr int E = SmElem<T>::E;
     __shared__ float2 sm[2][16];
     const size_t base = (size_t)blockIdx.x * cols;
-    const int nvec = cols / E, rest = nvec * E + threadIdx.x;
+    const int nvec = cols / E;
+    const int64_t rest = (int64_t)nvec * E + threadIdx.x;
     const float inv = 1.0f / (float)cols, tail = rest < cols ? SmElem<T>::load(x + base + rest) : 0.f;
     float s = tail, q = 0.f;
 #pragma unroll 4
@@ -284,7 +285,8 @@ __global__ __launch_bounds__(1024) void layer_norm_bwd_long(const T *x, const fl
     constexpr int E = SmElem<T>::E;
     __shared__ float2 sm[16];
     const size_t base = (size_t)blockIdx.x * cols;
-    const int nvec = cols / E, rest = nvec * E + threadIdx.x;
+    const int nvec = cols / E;
+    const int64_t rest = (int64_t)nvec * E + threadIdx.x;
     const float mu = mean[blockIdx.x], rs = rstd[blockIdx.x], inv = 1.0f / (float)cols;
     float2 s = make_float2(0.f, 0.f);
     float tg = 0.f, tx = 0.f;
@@ -407,17 +409,20 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_join(const float *__restri
     float *out = blockIdx.y ? dbeta : dgamma;
     if (!out) return;
     const int c = threadIdx.x & 31, q = threadIdx.x >> 5;
-    const int64_t j = (int64_t)blockIdx.x * 32 + c;
-    float s = 0.f;
-    if (j < cols)
+    for (int64_t j0 = (int64_t)blockIdx.x * 32; j0 < cols; j0 += (int64_t)gridDim.x * 32) {
+        const int64_t j = j0 + c;
+        float s = 0.f;
+        if (j < cols)
 #pragma unroll 8
-        for (int p = q; p < parts; p += 8) s += part[((size_t)p * 2 + blockIdx.y) * cols + j];
-    sm[q][c] = s;
-    __syncthreads();
-    if (q || j >= cols) return;
+            for (int p = q; p < parts; p += 8) s += part[((size_t)p * 2 + blockIdx.y) * cols + j];
+        __syncthreads();
+        sm[q][c] = s;
+        __syncthreads();
+        if (q || j >= cols) continue;
 #pragma unroll
-    for (int w = 1; w < 8; ++w) s += sm[w][c];
-    out[j] = s;
+        for (int w = 1; w < 8; ++w) s += sm[w][c];
+        out[j] = s;
+    }
 }
 
 // How rows of this length are taken: below one vector a thread per row; else the smallest group of lanes and the fewest vectors per lane that
@@ -546,7 +551,8 @@ static hipError_t launch_norm_bwd_t(int rows, int cols, const T *x, const float 
     }
     if (e != hipSuccess) return e;
     if (weights) {
-        NGC_LAUNCH(layer_norm_bwd_join, dim3((unsigned)(((int64_t)cols + 31) / 32), 2), dim3(256), 0, st, ws, dgamma, dbeta, parts, cols);
+        const int64_t tiles = ((int64_t)cols + 31) / 32;
+        NGC_LAUNCH(layer_norm_bwd_join, dim3((unsigned)(tiles < 65536 ? tiles : 65536), 2), dim3(256), 0, st, ws, dgamma, dbeta, parts, cols);
         if ((e = launch_result()) != hipSuccess) return e;
     }
     if (p.kernel == LN_TINY) {

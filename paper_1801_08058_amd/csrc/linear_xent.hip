@@ -402,6 +402,7 @@ static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int limbs, int most, 
     for (int edge = limbs == 3 || slab ? 128 : 256; edge >= 64; edge /= 2)
         for (int p : parts) {
             if (p > most || (p > 1 && k / p < 128)) break;
+            if (edge < 128 && ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * p > (1 << 22)) break;      // a grid holds fewer than 2^32 threads
             const float run = mm_expected(edge, limbs, m, n, stages, p), t = (run > bytes ? run : bytes) + (p > 1 || slab ? 3.f + (float)m * (float)n * 8.f * (float)p / 4e6f : 0.f);
             if (t < best.us && (!forced || atoi(forced) == edge || (slab && best.us == INFINITY))) best = {edge, p, t};
         }
@@ -468,10 +469,10 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
 
 static unsigned mm_grid(MmParams &mm, int edge)
 {
-    mm.mt = (mm.M + edge - 1) / edge;
-    mm.nt = (mm.N + edge - 1) / edge;
-    mm.kper = (int)up((mm.K + mm.splits - 1) / mm.splits, 32);
-    return (unsigned)(mm.mt * mm.nt * mm.splits);
+    mm.mt = (int)(((int64_t)mm.M + edge - 1) / edge);
+    mm.nt = (int)(((int64_t)mm.N + edge - 1) / edge);
+    mm.kper = (int)up(((int64_t)mm.K + mm.splits - 1) / mm.splits, 32);
+    return (unsigned)mm.mt * (unsigned)mm.nt * (unsigned)mm.splits;
 }
 
 template <typename T, int EDGE, bool AT, bool BT, XentEpilogue E>
@@ -550,9 +551,9 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
         }
         const int edge = copy_w || pl.piece == vocab ? pl.z.edge : mm_choose(rows, vocab, pl.pitch, pl.limbs, 1, false).edge;
         if ((e = launch_mm<T, false, false, XE_STATS>(p, edge, st)) != hipSuccess) return e;
-        tiles += (p.mm.N + edge - 1) / edge;
+        tiles += (int)(((int64_t)p.mm.N + edge - 1) / edge);
     }
-    NGC_LAUNCH(xent_join, dim3((rows + 31) / 32), dim3(256), 0, st, part, p.target, labels, loss, lse, rows, vocab, tiles);
+    NGC_LAUNCH(xent_join, dim3(((unsigned)rows + 31) / 32), dim3(256), 0, st, part, p.target, labels, loss, lse, rows, vocab, tiles);
     return launch_result();
 }
 

@@ -151,3 +151,21 @@ def test_results_do_not_depend_on_timing():
         got.append((loss, lse, dx, dw))
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+# every tile of the products at sizes that end inside it (the sizes alone would choose the smallest for most of them)
+@pytest.mark.parametrize("edge", [64, 128, 256])
+@pytest.mark.parametrize("dtype,rows,width,vocab", [("bf16", 1, 8, 2), ("bf16", 300, 96, 777), ("bf16", 257, 515, 1003), ("bf16", 640, 264, 5003), ("f32", 130, 72, 300),
+                                                    ("f32", 257, 515, 1003), ("bf16", 1100, 160, 3001)])
+def test_every_tile(monkeypatch, edge, dtype, rows, width, vocab):
+    print(f"linear_xent edge {edge} {rows} {width} {vocab} {dtype}", flush=True)
+    monkeypatch.setenv("NGC_XENT_TILE", str(edge))
+    _check(dtype, *_inputs(dtype, rows, width, vocab, 61 + rows))
+
+
+# few rows and classes, long rows: the product in parts and a workgroup per row
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width,vocab", [(1, 4096, 3), (128, 2048, 1000), (7, 3001, 257), (40, 1500, 4097), (1000, 2000, 5), (1025, 2000, 5)])
+def test_few_tiles_with_long_rows(dtype, rows, width, vocab):
+    print(f"linear_xent parts {rows} {width} {vocab} {dtype}", flush=True)
+    _check(dtype, *_inputs(dtype, rows, width, vocab, 71 + rows))
