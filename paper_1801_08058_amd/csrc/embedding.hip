@@ -153,21 +153,6 @@ __device__ __forceinline__ unsigned block_scan(unsigned v, unsigned *sm, unsigne
     return before + sum - v;
 }
 
-// Four elements at any element address as fp32
-template <typename T>
-__device__ __forceinline__ float4 load4_any(const T *p)
-{
-    if constexpr (sizeof(T) == 2) {
-        uint2 v;
-        __builtin_memcpy(&v, p, 8);
-        return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u));
-    } else {
-        float4 v;
-        __builtin_memcpy(&v, p, 16);
-        return v;
-    }
-}
-
 // First column of a lane's group of four; false past the end (the column is then 0).  The last group overlaps the one before it (both hold the
 // same sums).  ONE: a group is one column (widths below four).
 template <bool ONE>

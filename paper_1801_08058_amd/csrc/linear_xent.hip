@@ -41,6 +41,39 @@ __global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ la
     if (threadIdx.x == 0) *scale = top;
 }
 
+// Eight values as L limbs: the value rounded to bf16, what that leaves, rounded, and what that leaves (one limb: values that bf16 holds)
+template <int L>
+__device__ __forceinline__ void split_limbs(const float (&f)[8], mm_bf16x8 (&out)[L])
+{
+    float r[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r[k] = f[k];
+#pragma unroll
+    for (int q = 0; q < L; ++q) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            w[k] = pack_bf16x2_hw(r[2 * k], r[2 * k + 1]);
+            r[2 * k] -= __uint_as_float(w[k] << 16);
+            r[2 * k + 1] -= __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+        __builtin_memcpy(&out[q], w, 16);
+    }
+}
+// c + a b^T, of three limbs the six products that mm_bf16.h forms
+template <int L>
+__device__ __forceinline__ mm_f32x4 limb_products(const mm_bf16x8 (&a)[L], const mm_bf16x8 (&b)[L], mm_f32x4 c)
+{
+    if constexpr (L == 3) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[2], c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[2], b[0], c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1], b[1], c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[1], c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1], b[0], c, 0, 0, 0);
+    }
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[0], c, 0, 0, 0);
+}
+
 // T: uint16_t (bf16) or float (in limbs)
 enum XentEpilogue { XE_STATS, XE_GRAD, XE_SLAB, XE_OUT };
 
@@ -308,6 +341,244 @@ __global__ __launch_bounds__(256) void xent_row_grad(const float *__restrict__ s
     }
 }
 
+// ---- few rows, and a weight that the products above would have to copy (fp32, rows of no multiple of 16 bytes) ----
+//
+// The weight goes straight from memory to registers, at any alignment, and becomes limbs there: it is read once per product, where a copy
+// reads it, writes three bf16 values per element and reads those.  Bound: HBM.
+
+// Eight elements of a row, `left` of them inside it (the others are zero)
+template <typename T>
+struct Eight {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void load(const T *p, int left)
+    {
+        if (left >= 8) {
+            __builtin_memcpy(w, p, sizeof(w));
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (sizeof(T) == 4) w[k] = k < left ? __float_as_uint(p[k]) : 0u;
+            else if (k % 2 == 0) w[k / 2] = (k < left ? (uint32_t)p[k] : 0u) | (k + 1 < left ? (uint32_t)p[k + 1] << 16 : 0u);
+        }
+    }
+    template <int L> __device__ __forceinline__ void limbs(mm_bf16x8 (&out)[L]) const
+    {
+        if constexpr (L == 1) {
+            __builtin_memcpy(&out[0], w, 16);
+        } else {
+            float f[8];
+            __builtin_memcpy(f, w, 32);
+            split_limbs(f, out);
+        }
+    }
+};
+
+// z[m][v] of a wave's 32 classes and MT blocks of 16 rows.  x: copied, limbs xlimb elements apart
+template <typename T, int MT>
+__global__ __launch_bounds__(256) void xent_few_z(const uint16_t *__restrict__ x, int64_t xlimb, int pitch, const T *__restrict__ w, float *__restrict__ z, int ld,
+                                                  int rows, int width, int vocab)
+{
+    constexpr int L = sizeof(T) == 4 ? 3 : 1;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 32;
+    if (v0 >= vocab) return;
+    const T *row[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) row[i] = w + (size_t)(v0 + 16 * i + l < vocab ? v0 + 16 * i + l : vocab - 1) * width;
+    const uint16_t *xr[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) xr[j] = x + (size_t)(16 * j + l < rows ? 16 * j + l : rows - 1) * pitch;
+    mm_f32x4 acc[2][MT];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = mm_f32x4{0.f, 0.f, 0.f, 0.f};
+    auto products = [&](const Eight<T> (&raw)[2], int k) {
+        mm_bf16x8 a[2][L], b[MT][L];
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int q = 0; q < L; ++q) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (k < pitch) v = *reinterpret_cast<const uint4 *>(xr[j] + q * xlimb + k);             // zeros behind the row up to pitch
+                b[j][q] = __builtin_bit_cast(mm_bf16x8, v);
+            }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) raw[i].template limbs<L>(a[i]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[i][j] = limb_products(a[i], b[j], acc[i][j]);
+    };
+    // four steps of 32 elements under way at a time
+    constexpr int AHEAD = 4;
+    const int full = width / 32;
+    Eight<T> raw[AHEAD][2];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (u < full)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) raw[u][i].load(row[i] + 32 * u + 8 * g, 8);
+    for (int n = 0; n < full; n += AHEAD)
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (n + u >= full) break;
+            products(raw[u], 32 * (n + u) + 8 * g);
+            if (n + u + AHEAD < full)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) raw[u][i].load(row[i] + 32 * (n + u + AHEAD) + 8 * g, 8);
+        }
+    if (width % 32) {
+        const int k = 32 * full + 8 * g;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) raw[0][i].load(row[i] + (k < width ? k : 0), k < width ? width - k : 0);     // lanes past the row read nothing
+        products(raw[0], k);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            const int m = 16 * j + l, v = v0 + 16 * i + 4 * g;
+            if (m < rows && v < ld) *reinterpret_cast<mm_f32x4 *>(z + (size_t)m * ld + v) = acc[i][j];
+        }
+}
+
+// dx[m][d] = sum_v g[m][v] w[v][d] of 64 columns and MT blocks of 16 rows over the classes of part blockIdx.y: a slab.  The four waves take every
+// fourth step of 32 classes and are added up through LDS.  Column 4 r + c is row r of fragment c, so that a lane loads four columns of a class.
+template <typename T, int MT>
+__global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ gr, int64_t glimb, int gp, const T *__restrict__ w, float *__restrict__ slab,
+                                                   int pitch, int rows, int width, int vocab, int per_part)
+{
+    constexpr int L = sizeof(T) == 4 ? 3 : 1;
+    __shared__ mm_f32x4 sums[3][4 * MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
+    const int d = blockIdx.x * 64 + 4 * l, end = per_part * (blockIdx.y + 1) < vocab ? per_part * (blockIdx.y + 1) : vocab;
+    mm_f32x4 acc[4][MT];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[c][j] = mm_f32x4{0.f, 0.f, 0.f, 0.f};
+    const uint16_t *xr[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) xr[j] = gr + (size_t)(16 * j + l < rows ? 16 * j + l : rows - 1) * gp;
+    struct Block {
+        float4 q[8];
+    };
+    auto load = [&](Block &blk, int v0) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int v = v0 + 8 * g + k < vocab ? v0 + 8 * g + k : vocab - 1;                          // g is zero past the classes
+            const T *p = w + (size_t)v * width + d;
+            float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (d + 4 <= width) {
+                q = load4_any(p);
+            } else {
+                if (d < width) q.x = SmElem<T>::load(p);
+                if (d + 1 < width) q.y = SmElem<T>::load(p + 1);
+                if (d + 2 < width) q.z = SmElem<T>::load(p + 2);
+            }
+            blk.q[k] = q;
+        }
+    };
+    const int begin = per_part * blockIdx.y + 32 * wave;
+    Block now, next;
+    if (begin < end) load(next, begin);
+    for (int v0 = begin; v0 < end; v0 += 128) {
+        now = next;
+        if (v0 + 128 < end) load(next, v0 + 128);
+        mm_bf16x8 b[MT][L];
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int q = 0; q < L; ++q) b[j][q] = *reinterpret_cast<const mm_bf16x8 *>(xr[j] + q * glimb + v0 + 8 * g);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = c == 0 ? now.q[k].x : c == 1 ? now.q[k].y : c == 2 ? now.q[k].z : now.q[k].w;
+            mm_bf16x8 a[L];
+            split_limbs(f, a);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[c][j] = limb_products(a, b[j], acc[c][j]);
+        }
+    }
+    if (wave)
+#pragma unroll
+        for (int q = 0; q < 4 * MT; ++q) sums[wave - 1][q][lane] = acc[q / MT][q % MT];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int q = 0; q < 4 * MT; ++q) acc[q / MT][q % MT] += sums[s][q][lane];
+    float *out = slab + (size_t)blockIdx.y * rows * pitch;
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int m = 16 * j + l, at = blockIdx.x * 64 + 16 * g + 4 * e;
+            if (m < rows && at < pitch) *reinterpret_cast<mm_f32x4 *>(out + (size_t)m * pitch + at) = mm_f32x4{acc[0][j][e], acc[1][j][e], acc[2][j][e], acc[3][j][e]};
+        }
+}
+
+// dw[v][d] = scale sum_m g[m][v] x[m][d] of at most 16 rows: every thread keeps four columns of x and stores them for class after class.  A
+// workgroup takes 1024 columns of `classes` classes, their g in LDS.
+template <typename T>
+__global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ gr, int64_t glimb, int gp, const T *__restrict__ x, const float *__restrict__ scale,
+                                                   T *__restrict__ dw, int rows, int width, int vocab)
+{
+    constexpr int CLASSES = 64;
+    __shared__ float gs[CLASSES][16];
+    const int v0 = blockIdx.x * CLASSES, d = (blockIdx.y * 256 + threadIdx.x) * 4;
+    const float sc = *scale;
+    for (int i = threadIdx.x; i < CLASSES * 16; i += 256) {
+        const int v = i % CLASSES, m = i / CLASSES;
+        float s = 0.f;
+        if (m < rows)
+#pragma unroll
+            for (int q = (sizeof(T) == 4 ? 3 : 1) - 1; q >= 0; --q) s += bf16_bits_to_float(gr[q * glimb + (size_t)m * gp + v0 + v]);        // gp is a multiple of 64
+        gs[v][m] = s * sc;
+    }
+    float4 f[16];
+#pragma unroll
+    for (int m = 0; m < 16; ++m) {
+        f[m] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const T *p = x + (size_t)m * width + d;
+        if (m >= rows) continue;
+        if (d + 4 <= width) {
+            f[m] = load4_any(p);
+        } else {
+            if (d < width) f[m].x = SmElem<T>::load(p);
+            if (d + 1 < width) f[m].y = SmElem<T>::load(p + 1);
+            if (d + 2 < width) f[m].z = SmElem<T>::load(p + 2);
+        }
+    }
+    __syncthreads();
+    const int end = vocab - v0 < CLASSES ? vocab - v0 : CLASSES;
+    for (int v = 0; v < end; ++v) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int m = 0; m < 16; ++m) {
+            const float g = gs[v][m];
+            s.x = fmaf(g, f[m].x, s.x), s.y = fmaf(g, f[m].y, s.y), s.z = fmaf(g, f[m].z, s.z), s.w = fmaf(g, f[m].w, s.w);
+        }
+        T *at = dw + (size_t)(v0 + v) * width + d;
+        if (d + 4 <= width) {
+            if constexpr (sizeof(T) == 4) {
+                store16_any(at, make_uint4(__float_as_uint(s.x), __float_as_uint(s.y), __float_as_uint(s.z), __float_as_uint(s.w)));
+            } else {
+                const uint2 b = make_uint2(pack_bf16x2_hw(s.x, s.y), pack_bf16x2_hw(s.z, s.w));
+                __builtin_memcpy(at, &b, 8);
+            }
+        } else {
+            if (d < width) SmElem<T>::store(at, s.x);
+            if (d + 1 < width) SmElem<T>::store(at + 1, s.y);
+            if (d + 2 < width) SmElem<T>::store(at + 2, s.z);
+        }
+    }
+}
+
 // lse and loss of 32 rows from the tiles' maxima and sums, eight parts of the tiles each
 __global__ __launch_bounds__(256) void xent_join(const float2 *__restrict__ part, const float *__restrict__ target, const int64_t *__restrict__ labels,
                                                   float *__restrict__ loss, float *__restrict__ lse, int rows, int vocab, int tiles)
@@ -416,10 +687,17 @@ struct XentPlan {
     int64_t krows;               // rows as the products count them where they are the reduction
     MmChoice z, dx, dw;          // products of a whole piece
     bool by_rows;                // z in slabs, then a workgroup per row
+    bool few;                    // by_rows with the weight straight from memory; dx as well, in dx.splits parts
     size_t info, scale, zslab, xcopy, wcopy, g, dx_slab, dw_slab, total; // offsets in the workspace
 };
 
 static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
+
+// Rows that the kernels for few rows take, 16, 32 or 64 a workgroup; more would read the weight again
+// (107 x 1921 over 33171 classes bf16: 189 us against 128 with copies).  Fewer than 8192 classes are fewer than 256 waves, and their copy is short
+// (128 x 2048 over 1000 classes fp32: 121 against 25 us).
+constexpr int XENT_FEW = 64, XENT_FEW_VOCAB = 8192;
+static int few_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 
 static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bwd)
 {
@@ -448,6 +726,17 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         p.by_rows = parts.us < p.z.us && (int64_t)rows * up(vocab, 8) * 4 * parts.splits <= (32 << 20);
         if (p.by_rows) p.z = parts;
     }
+    if (p.copy && rows <= XENT_FEW && vocab >= XENT_FEW_VOCAB && (int64_t)rows * up(vocab, 8) * 4 <= (64 << 20) && vocab <= (1 << 21)) {
+        p.few = p.by_rows = true;
+        p.piece = vocab;
+        p.z = {64, 1, 0.f};
+        // about 1024 workgroups, parts of at least 512 classes
+        const int blocks = (int)((width + 63) / 64), most = (int)((vocab + 511) / 512);
+        p.dx = {64, 1024 / blocks < 1 ? 1 : 1024 / blocks, 0.f};
+        if (p.dx.splits > most) p.dx.splits = most;
+        if (p.dx.splits > 64) p.dx.splits = 64;
+        if (bwd) p.dw = mm_choose(vocab, p.pitch, rows, p.limbs, 1, false);
+    }
     size_t at = 0;
     auto take = [&](size_t &where, size_t bytes) { where = at; at += r256(bytes); };
     if (p.by_rows) take(p.zslab, (size_t)rows * up(vocab, 8) * 4 * p.z.splits);
@@ -462,7 +751,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         take(p.dw_slab, p.dw.splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw.splits : 0);
     }
     take(p.xcopy, (size_t)p.krows * p.pitch * 2 * p.limbs);
-    take(p.wcopy, (size_t)up(p.piece, 32) * p.pitch * 2 * p.limbs);
+    if (!p.few) take(p.wcopy, (size_t)up(p.piece, 32) * p.pitch * 2 * p.limbs);
     p.total = at;
     return p;
 }
@@ -506,6 +795,28 @@ static hipError_t launch_both(XentMm dx, XentMm dw, hipStream_t st)
     return launch_result();
 }
 
+// z of all classes into a slab
+template <typename T>
+static hipError_t launch_few_z(const uint16_t *x, int64_t xlimb, int pitch, const T *w, float *z, int rows, int width, int vocab, hipStream_t st)
+{
+    const dim3 grid((unsigned)((vocab + 127) / 128));
+    const int ld = (int)up(vocab, 8), mt = few_tiles(rows);
+    const auto kernel = mt == 1 ? xent_few_z<T, 1> : mt == 2 ? xent_few_z<T, 2> : xent_few_z<T, 4>;
+    NGC_LAUNCH(kernel, grid, dim3(256), 0, st, x, xlimb, pitch, w, z, ld, rows, width, vocab);
+    return launch_result();
+}
+
+template <typename T>
+static hipError_t launch_few_dx(const uint16_t *g, int64_t glimb, int gp, const T *w, float *slab, int pitch, int rows, int width, int vocab, int splits,
+                                hipStream_t st)
+{
+    const dim3 grid((unsigned)((width + 63) / 64), (unsigned)splits);
+    const int per = (int)up(((int64_t)vocab + splits - 1) / splits, 128), mt = few_tiles(rows);
+    const auto kernel = mt == 1 ? xent_few_dx<T, 1> : mt == 2 ? xent_few_dx<T, 2> : xent_few_dx<T, 4>;
+    NGC_LAUNCH(kernel, grid, dim3(256), 0, st, g, glimb, gp, w, slab, pitch, rows, width, vocab, per);
+    return launch_result();
+}
+
 // x or rows of w as the products read them: where they are, or a copy.  all: rows of the copy
 template <typename T>
 static hipError_t operand(const XentPlan &pl, const T *src, char *copy, int64_t rows, int64_t all, int width, const uint16_t *&out, hipStream_t st)
@@ -532,6 +843,13 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
     p.vocab = vocab; p.labels = labels;
     p.target = reinterpret_cast<float *>(ws + pl.scale);
     float2 *part = reinterpret_cast<float2 *>(ws + pl.info);
+    if (pl.few) {
+        float *z = reinterpret_cast<float *>(ws + pl.zslab);
+        const int ld = (int)up(vocab, 8);
+        if ((e = launch_few_z(p.mm.a, p.mm.alimb, pl.pitch, w, z, rows, width, vocab, st)) != hipSuccess) return e;
+        NGC_LAUNCH(xent_row_loss, dim3(rows), dim3(256), 0, st, z, 1, (size_t)0, ld, labels, loss, lse, vocab);
+        return launch_result();
+    }
     int tiles = 0;
     for (int64_t v0 = 0; v0 < vocab; v0 += p.mm.N) {
         const int64_t left = vocab - v0;
@@ -577,12 +895,13 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
     if (!pl.by_rows && (e = launch_result()) != hipSuccess) return e;
     const uint16_t *xp, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
     if ((e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
-    const bool one = pl.piece >= vocab && pl.dx.splits == 1;             // dx leaves the products whole
-    const bool together = dx && dw && pl.dw.splits == 1 && pl.dx.edge == pl.dw.edge && pl.dw.edge < 256;
+    const bool one = pl.piece >= vocab && pl.dx.splits == 1 && !pl.few;  // dx leaves the products whole
+    const bool together = dx && dw && !pl.few && pl.dw.splits == 1 && pl.dx.edge == pl.dw.edge && pl.dw.edge < 256;
     for (int64_t v0 = 0; v0 < vocab; v0 += pl.piece) {
         const int piece = vocab - v0 < pl.piece ? (int)(vocab - v0) : pl.piece, gp = (int)up(piece, 64);
         const int kpiece = (int)(pl.limbs == 3 ? up(piece, 32) : piece);
-        if ((e = operand(pl, w + (size_t)v0 * width, ws + pl.wcopy, piece, kpiece, width, wp, st)) != hipSuccess) return e;
+        if (pl.few) wp = nullptr;                                        // w is read where it is
+        else if ((e = operand(pl, w + (size_t)v0 * width, ws + pl.wcopy, piece, kpiece, width, wp, st)) != hipSuccess) return e;
         XentMm p{};
         p.v0 = (int)v0; p.vocab = vocab; p.info = info; p.scale = scale;
         p.mm.a = xp; p.mm.b = wp;
@@ -596,7 +915,8 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             q.slab = reinterpret_cast<float *>(ws + pl.zslab);
             q.ldo = q.store_n = ld; q.store_m = rows;
             q.mm.splits = pl.z.splits;
-            if ((e = launch_mm<T, false, false, XE_SLAB>(q, pl.z.edge, st)) != hipSuccess) return e;
+            e = pl.few ? launch_few_z(xp, q.mm.alimb, pl.pitch, w, q.slab, rows, width, vocab, st) : launch_mm<T, false, false, XE_SLAB>(q, pl.z.edge, st);
+            if (e != hipSuccess) return e;
             NGC_LAUNCH((xent_row_grad<T>), dim3((unsigned)pl.krows), dim3(256), 0, st, q.slab, pl.z.splits, (size_t)rows * ld, ld, labels, lse, dloss,
                        reinterpret_cast<uint16_t *>(ws + pl.g), p.glimb, gp, scale, rows, vocab);
             e = launch_result();
@@ -605,7 +925,9 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
         }
         if (e != hipSuccess) return e;
         XentMm both{};                                                   // dx, while it waits to run together with dw
-        if (dx) {
+        if (dx && pl.few) {
+            if ((e = launch_few_dx(g, p.glimb, gp, w, dx_slab, pl.pitch, rows, width, vocab, pl.dx.splits, st)) != hipSuccess) return e;
+        } else if (dx) {
             XentMm q = p;
             q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
             q.mm.M = rows; q.mm.N = pl.pitch; q.mm.K = kpiece; q.mm.splits = pl.dx.splits;
@@ -620,7 +942,11 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             if (e != hipSuccess) return e;
             both = q;
         }
-        if (dw) {
+        if (dw && pl.few && rows <= 16) {
+            NGC_LAUNCH((xent_few_dw<T>), dim3((unsigned)((vocab + 63) / 64), (unsigned)((width + 1023) / 1024)), dim3(256), 0, st, g, p.glimb, gp, x, scale, dw, rows,
+                       width, vocab);
+            if ((e = launch_result()) != hipSuccess) return e;
+        } else if (dw) {
             XentMm q = p;
             q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
             q.mm.b = xp; q.mm.blimb = pl.krows * pl.pitch;

@@ -90,6 +90,21 @@ __device__ __forceinline__ void store16_any(T *p, uint4 v)
     __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any *>(p));
 }
 
+// Four elements at any element address as fp32
+template <typename T>
+__device__ __forceinline__ float4 load4_any(const T *p)
+{
+    if constexpr (sizeof(T) == 2) {
+        uint2 v;
+        __builtin_memcpy(&v, p, 8);
+        return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u));
+    } else {
+        float4 v;
+        __builtin_memcpy(&v, p, 16);
+        return v;
+    }
+}
+
 // Vectors that stay packed over several passes: what was unpacked of them before this point is unpacked again after it instead of being kept
 // in registers.
 template <int N> __device__ __forceinline__ void keep_packed(uint4 (&v)[N])

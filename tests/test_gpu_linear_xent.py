@@ -169,3 +169,13 @@ def test_every_tile(monkeypatch, edge, dtype, rows, width, vocab):
 def test_few_tiles_with_long_rows(dtype, rows, width, vocab):
     print(f"linear_xent parts {rows} {width} {vocab} {dtype}", flush=True)
     _check(dtype, *_inputs(dtype, rows, width, vocab, 71 + rows))
+
+
+# few rows whose weight has to be read where it is (fp32, or rows off the 16-byte grid) over many classes
+@pytest.mark.parametrize("dtype,rows,width,vocab", [("f32", 1, 64, 8192), ("f32", 5, 860, 9001), ("f32", 16, 33, 20011), ("f32", 17, 100, 8199), ("f32", 33, 7, 8300),
+                                                    ("f32", 64, 130, 8205), ("f32", 65, 130, 8205), ("bf16", 1, 1, 8192), ("bf16", 3, 515, 10007), ("bf16", 16, 1030, 8193),
+                                                    ("bf16", 40, 67, 8221), ("bf16", 64, 129, 9000), ("f32", 2, 5, 8191)])
+def test_few_rows_over_many_classes(dtype, rows, width, vocab):
+    print(f"linear_xent few {rows} {width} {vocab} {dtype}", flush=True)
+    _check(dtype, *_inputs(dtype, rows, width, vocab, 81 + rows))
+    _check(dtype, *_inputs(dtype, rows, width, vocab, 82 + rows), offset=1)
