@@ -29,14 +29,33 @@ __global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ la
                                                   XentRow *__restrict__ info, float *__restrict__ scale, int rows, int vocab)
 {
     __shared__ float sm[16];
-    float top = 0.f;
-    for (int m = threadIdx.x; m < rows; m += 1024)
-        if (labels[m] >= 0 && labels[m] < vocab) top = fmaxf(top, fabsf(dloss[m]));
+    constexpr int B = 8;                                                 // rows of a thread whose loads are under way together
+    int64_t label[B];
+    float weight[B], l[B], top = 0.f;
+    auto load = [&](int m0) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const int m = m0 + 1024 * b + threadIdx.x;
+            label[b] = -1;
+            if (m < rows) label[b] = labels[m], weight[b] = dloss[m], l[b] = lse[m];
+            if (label[b] >= vocab) label[b] = -1;
+        }
+    };
+    for (int m0 = 0; m0 < rows; m0 += 1024 * B) {
+        load(m0);
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            if (label[b] >= 0) top = fmaxf(top, fabsf(weight[b]));
+    }
     top = fmaxf(block_reduce<16>(top, true, sm), 0x1p-100f);             // all zero: any scale
     const float inv = 1.0f / top;
-    for (int m = threadIdx.x; m < rows; m += 1024) {
-        const bool live = labels[m] >= 0 && labels[m] < vocab;
-        info[m] = XentRow{lse[m] * LOG2E, live ? dloss[m] * inv : 0.f, live ? (int)labels[m] : -1, 0};
+    for (int m0 = 0; m0 < rows; m0 += 1024 * B) {
+        if (rows > 1024 * B) load(m0);
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const int m = m0 + 1024 * b + threadIdx.x;
+            if (m < rows) info[m] = XentRow{l[b] * LOG2E, label[b] >= 0 ? weight[b] * inv : 0.f, label[b] >= 0 ? (int)label[b] : -1, 0};
+        }
     }
     if (threadIdx.x == 0) *scale = top;
 }
@@ -89,7 +108,7 @@ struct XentMm {
     int64_t ldo, glimb;
     int store_m, store_n;                // rows and columns that are stored (GRAD: zeros past the rows and the piece)
     float *slab;                         // SLAB: [splits][M][ldo]
-    int add;                             // SLAB: onto what is there
+    int add;                             // SLAB: onto what is there; OUT: the slab ([M][N]) joins the result
 };
 
 template <typename T, int BM, int BN, bool AT, bool BT, XentEpilogue E>
@@ -201,7 +220,11 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < FN; ++i) acc[i][j] *= scale;
+            for (int i = 0; i < FN; ++i) {
+                const int n = n_ + 16 * i;
+                if (p.add && m < p.store_m && n < p.mm.N) acc[i][j] += *reinterpret_cast<const mm_f32x4 *>(p.slab + (size_t)m * p.mm.N + n);
+                acc[i][j] *= scale;
+            }
         }
         if constexpr (E == XE_OUT && LIMBS) {
             if (m >= p.store_m) continue;
@@ -274,69 +297,109 @@ __global__ __launch_bounds__(64 * MM_WAVES) void xent_mm_both(const XentMm dx, c
 // Few tiles: the logits' product runs in parts (fp32 slabs, `stride` elements apart, rows of `ld`), and a workgroup per row adds them up.
 __device__ __forceinline__ mm_f32x4 sum_parts(const float *at, int splits, size_t stride)
 {
+    constexpr int B = 8;                                                         // parts under way together, added in their order
     mm_f32x4 v = *reinterpret_cast<const mm_f32x4 *>(at);
+    int q = 1;
+    for (; q + B <= splits; q += B) {
+        mm_f32x4 f[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) f[b] = *reinterpret_cast<const mm_f32x4 *>(at + (q + b) * stride);
+#pragma unroll
+        for (int b = 0; b < B; ++b) v += f[b];
+    }
 #pragma unroll 4
-    for (int q = 1; q < splits; ++q) v += *reinterpret_cast<const mm_f32x4 *>(at + q * stride);
+    for (; q < splits; ++q) v += *reinterpret_cast<const mm_f32x4 *>(at + q * stride);
     return v;
 }
 
-__global__ __launch_bounds__(256) void xent_row_loss(const float *__restrict__ slab, int splits, size_t stride, int ld, const int64_t *__restrict__ labels,
-                                                     float *__restrict__ loss, float *__restrict__ lse, int vocab)
+constexpr int XENT_BATCH = 4;                                            // groups of four classes of a thread under way together
+
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void xent_row_loss(const float *__restrict__ slab, int splits, size_t stride, int ld, const int64_t *__restrict__ labels,
+                                                         float *__restrict__ loss, float *__restrict__ lse, int vocab)
 {
-    __shared__ float sm[4], target;
+    __shared__ float sm[NW], target;
     const int m = blockIdx.x;
     const int64_t label = labels[m];
     const bool live = label >= 0 && label < vocab;
     float top = -INFINITY, s = 0.f;
-    for (int v = threadIdx.x * 4; v < vocab; v += 1024) {
-        const mm_f32x4 z = sum_parts(slab + (size_t)m * ld + v, splits, stride);
+    for (int w0 = 0; w0 < vocab; w0 += 256 * NW * XENT_BATCH) {
+        const int v0 = w0 + threadIdx.x * 4;
+        mm_f32x4 z[XENT_BATCH];
+#pragma unroll
+        for (int b = 0; b < XENT_BATCH; ++b) {
+            if (w0 + 256 * NW * b >= vocab) break;
+            const int v = v0 + 256 * NW * b;
+            z[b] = sum_parts(slab + (size_t)m * ld + (v < vocab ? v : 0), splits, stride);
+        }
         float up = top;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (v + e < vocab) {
-                up = fmaxf(up, z[e] * LOG2E);
-                if (label == v + e) target = z[e];
+        for (int b = 0; b < XENT_BATCH; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int v = v0 + 256 * NW * b + e;
+                if (v >= vocab) z[b][e] = -INFINITY;                             // groups that were not loaded among them
+                up = fmaxf(up, z[b][e]);
+                if (label == v && live) target = z[b][e];
             }
-        s *= __builtin_amdgcn_exp2f(top - up);                                   // 0 the first time
+        s *= __builtin_amdgcn_exp2f((top - up) * LOG2E);                         // 0 the first time
         top = up;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += v + e < vocab ? __builtin_amdgcn_exp2f(fmaf(z[e], LOG2E, -top)) : 0.f;
+        for (int b = 0; b < XENT_BATCH; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((z[b][e] - top) * LOG2E);
     }
-    const float all = block_reduce<4>(top, true, sm);
-    s = block_reduce<4>(top == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f(top - all), false, sm);
+    const float all = block_reduce<NW>(top, true, sm);
+    s = block_reduce<NW>(top == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f((top - all) * LOG2E), false, sm);
     if (threadIdx.x) return;
-    const float l = (all + log2f(s)) * LN2;
+    const float l = all + log2f(s) * LN2;
     lse[m] = l;
     loss[m] = live ? l - target : 0.f;
 }
 
 // g of a row, as xent_rows and the epilogue of the product form it; rows from `rows` on are zeros.  Workgroup 0 leaves the scale.
-template <typename T>
-__global__ __launch_bounds__(256) void xent_row_grad(const float *__restrict__ slab, int splits, size_t stride, int ld, const int64_t *__restrict__ labels,
-                                                     const float *__restrict__ lse, const float *__restrict__ dloss, uint16_t *__restrict__ g,
-                                                     int64_t glimb, int gp, float *__restrict__ scale, int rows, int vocab)
+template <typename T, int NW>
+__global__ __launch_bounds__(64 * NW) void xent_row_grad(const float *__restrict__ slab, int splits, size_t stride, int ld, const int64_t *__restrict__ labels,
+                                                         const float *__restrict__ lse, const float *__restrict__ dloss, uint16_t *__restrict__ g,
+                                                         int64_t glimb, int gp, float *__restrict__ scale, int rows, int vocab)
 {
-    __shared__ float sm[4];
+    __shared__ float sm[NW];
     const int m = blockIdx.x;
     float most = 0.f;
-    for (int r = threadIdx.x; r < rows; r += 256)
-        if (labels[r] >= 0 && labels[r] < vocab) most = fmaxf(most, fabsf(dloss[r]));
-    most = fmaxf(block_reduce<4>(most, true, sm), 0x1p-100f);
+#pragma unroll 4
+    for (int r = threadIdx.x; r < rows; r += 64 * NW) {
+        const int64_t label = labels[r];
+        const float weight = fabsf(dloss[r]);
+        most = fmaxf(most, label >= 0 && label < vocab ? weight : 0.f);
+    }
+    most = fmaxf(block_reduce<NW>(most, true, sm), 0x1p-100f);
     if (m == 0 && threadIdx.x == 0) *scale = most;
     const int64_t label = m < rows ? labels[m] : -1;
     const bool live = label >= 0 && label < vocab;
     const float factor = live ? dloss[m] * (1.0f / most) : 0.f, lse2 = live ? lse[m] * LOG2E : 0.f;
-    for (int v = threadIdx.x * 4; v < gp; v += 1024) {
-        mm_f32x4 z = mm_f32x4{0.f, 0.f, 0.f, 0.f};
-        if (live && v < vocab) z = sum_parts(slab + (size_t)m * ld + v, splits, stride);
+    const size_t row = (size_t)(live ? m : 0) * ld;
+    for (int w0 = 0; w0 < gp; w0 += 256 * NW * XENT_BATCH) {
+        const int v0 = w0 + threadIdx.x * 4;
+        mm_f32x4 z[XENT_BATCH];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            z[e] = live && v + e < vocab ? __builtin_amdgcn_exp2f(fmaf(z[e], LOG2E, -lse2)) * factor - (label == v + e ? factor : 0.f) : 0.f;
+        for (int b = 0; b < XENT_BATCH; ++b) {
+            if (w0 + 256 * NW * b >= gp) break;
+            const int v = v0 + 256 * NW * b;
+            z[b] = sum_parts(slab + row + (v < vocab ? v : 0), splits, stride);
+        }
 #pragma unroll
-        for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
-            const uint2 b = make_uint2(pack_bf16x2_hw(z[0], z[1]), pack_bf16x2_hw(z[2], z[3]));
-            *reinterpret_cast<uint2 *>(g + l * glimb + (size_t)m * gp + v) = b;
-            z -= mm_f32x4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xFFFF0000u), __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xFFFF0000u)};
+        for (int b = 0; b < XENT_BATCH; ++b) {
+            const int v = v0 + 256 * NW * b;
+            if (v >= gp) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                z[b][e] = live && v + e < vocab ? __builtin_amdgcn_exp2f(fmaf(z[b][e], LOG2E, -lse2)) * factor - (label == v + e ? factor : 0.f) : 0.f;
+#pragma unroll
+            for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
+                const uint2 q = make_uint2(pack_bf16x2_hw(z[b][0], z[b][1]), pack_bf16x2_hw(z[b][2], z[b][3]));
+                *reinterpret_cast<uint2 *>(g + l * glimb + (size_t)m * gp + v) = q;
+                z[b] -= mm_f32x4{__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xFFFF0000u), __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xFFFF0000u)};
+            }
         }
     }
 }
@@ -465,20 +528,30 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
     struct Block {
         float4 q[8];
     };
+    // A lane whose four columns end behind the row loads the row's last four, of which the later products take what is theirs (shift); all loads of
+    // a block are under way together
+    const int from = d + 4 <= width ? d : width - 4, shift = d - from;
     auto load = [&](Block &blk, int v0) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int v = v0 + 8 * g + k < vocab ? v0 + 8 * g + k : vocab - 1;                          // g is zero past the classes
-            const T *p = w + (size_t)v * width + d;
-            float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (d + 4 <= width) {
-                q = load4_any(p);
+            const T *p = w + (size_t)v * width;
+            if (width >= 4) {
+                blk.q[k] = load4_any(p + from);
             } else {
-                if (d < width) q.x = SmElem<T>::load(p);
-                if (d + 1 < width) q.y = SmElem<T>::load(p + 1);
-                if (d + 2 < width) q.z = SmElem<T>::load(p + 2);
+                blk.q[k] = make_float4(SmElem<T>::load(p), width > 1 ? SmElem<T>::load(p + 1) : 0.f, width > 2 ? SmElem<T>::load(p + 2) : 0.f, 0.f);
             }
-            blk.q[k] = q;
+        }
+    };
+    const bool edge = width < 4 ? l != 0 : shift != 0;
+    auto own_columns = [&](Block &blk) {
+        if (!__any(edge)) return;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float4 q = blk.q[k];
+            if (!edge) continue;
+            blk.q[k] = width < 4 || shift > 3 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                              : make_float4(shift == 1 ? q.y : shift == 2 ? q.z : q.w, shift == 1 ? q.z : shift == 2 ? q.w : 0.f, shift == 1 ? q.w : 0.f, 0.f);
         }
     };
     const int begin = per_part * blockIdx.y + 32 * wave;
@@ -487,6 +560,7 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
     for (int v0 = begin; v0 < end; v0 += 128) {
         now = next;
         if (v0 + 128 < end) load(next, v0 + 128);
+        own_columns(now);
         mm_bf16x8 b[MT][L];
 #pragma unroll
         for (int j = 0; j < MT; ++j)
@@ -522,15 +596,15 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
         }
 }
 
-// dw[v][d] = scale sum_m g[m][v] x[m][d] of at most 16 rows: every thread keeps four columns of x and stores them for class after class.  A
-// workgroup takes 1024 columns of `classes` classes, their g in LDS.
-template <typename T>
+// dw[v][d] = scale sum_m g[m][v] x[m][d] of at most 16 rows: a thread keeps four columns of x and stores them for class after class.  A workgroup
+// takes 64 classes, their g in LDS, and 4 LPR columns; 256 / LPR classes at a time.
+template <typename T, int LPR>
 __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ gr, int64_t glimb, int gp, const T *__restrict__ x, const float *__restrict__ scale,
                                                    T *__restrict__ dw, int rows, int width, int vocab)
 {
     constexpr int CLASSES = 64;
     __shared__ float gs[CLASSES][16];
-    const int v0 = blockIdx.x * CLASSES, d = (blockIdx.y * 256 + threadIdx.x) * 4;
+    const int v0 = blockIdx.x * CLASSES, d = (blockIdx.y * LPR + (threadIdx.x & (LPR - 1))) * 4;
     const float sc = *scale;
     for (int i = threadIdx.x; i < CLASSES * 16; i += 256) {
         const int v = i % CLASSES, m = i / CLASSES;
@@ -543,20 +617,15 @@ __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ 
     float4 f[16];
 #pragma unroll
     for (int m = 0; m < 16; ++m) {
-        f[m] = make_float4(0.f, 0.f, 0.f, 0.f);
-        const T *p = x + (size_t)m * width + d;
-        if (m >= rows) continue;
-        if (d + 4 <= width) {
-            f[m] = load4_any(p);
-        } else {
-            if (d < width) f[m].x = SmElem<T>::load(p);
-            if (d + 1 < width) f[m].y = SmElem<T>::load(p + 1);
-            if (d + 2 < width) f[m].z = SmElem<T>::load(p + 2);
-        }
+        const T *p = x + (size_t)(m < rows ? m : 0) * width;
+        auto at = [&](int c) { return m < rows && c < width ? SmElem<T>::load(p + c) : 0.f; };
+        if (d + 4 <= width && m < rows) f[m] = load4_any(p + d);
+        else f[m] = make_float4(at(d), at(d + 1), at(d + 2), at(d + 3));
     }
     __syncthreads();
     const int end = vocab - v0 < CLASSES ? vocab - v0 : CLASSES;
-    for (int v = 0; v < end; ++v) {
+    if (d >= width) return;
+    for (int v = threadIdx.x / LPR; v < end; v += 256 / LPR) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int m = 0; m < 16; ++m) {
@@ -572,7 +641,7 @@ __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ 
                 __builtin_memcpy(at, &b, 8);
             }
         } else {
-            if (d < width) SmElem<T>::store(at, s.x);
+            SmElem<T>::store(at, s.x);
             if (d + 1 < width) SmElem<T>::store(at + 1, s.y);
             if (d + 2 < width) SmElem<T>::store(at + 2, s.z);
         }
@@ -587,10 +656,16 @@ __global__ __launch_bounds__(256) void xent_join(const float2 *__restrict__ part
     const int r = threadIdx.x & 31, q = threadIdx.x >> 5, m = blockIdx.x * 32 + r;
     float top = -INFINITY, s = 0.f;
     if (m < rows)
-        for (int t = q; t < tiles; t += 8) {
-            const float2 v = part[(size_t)t * rows + m];
-            const float up = fmaxf(top, v.x);
-            s = s * __builtin_amdgcn_exp2f(top - up) + v.y * __builtin_amdgcn_exp2f(v.x - up);
+        for (int t0 = q; t0 < tiles; t0 += 32) {
+            float2 v[4];                                                         // four tiles at a time; the first has a finite maximum
+#pragma unroll
+            for (int b = 0; b < 4; ++b) v[b] = t0 + 8 * b < tiles ? part[(size_t)(t0 + 8 * b) * rows + m] : make_float2(-INFINITY, 0.f);
+            float up = top;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) up = fmaxf(up, v[b].x);
+            s *= __builtin_amdgcn_exp2f(top - up);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) s += v[b].y * __builtin_amdgcn_exp2f(v[b].x - up);
             top = up;
         }
     red[q][r] = make_float2(top, s);
@@ -637,8 +712,7 @@ __global__ __launch_bounds__(256) void xent_sum(const float *__restrict__ slab, 
     if (j >= width) return;
     const float s = *scale;
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        mm_f32x4 v = mm_f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int q = 0; q < splits; ++q) v += *reinterpret_cast<const mm_f32x4 *>(slab + ((size_t)q * rows + r) * pitch + j);
+        const mm_f32x4 v = sum_parts(slab + (size_t)r * pitch + j, splits, (size_t)rows * pitch);
         for (int e = 0; e < 4 && j + e < width; ++e) SmElem<T>::store(out + (size_t)r * width + j + e, v[e] * s);
     }
 }
@@ -747,7 +821,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         take(p.info, (size_t)rows * sizeof(XentRow));
         take(p.scale, 4);
         take(p.g, (size_t)p.krows * up(p.piece, 64) * 2 * p.limbs);
-        take(p.dx_slab, (size_t)rows * p.pitch * 4 * p.dx.splits);
+        take(p.dx_slab, p.dx.splits > 1 || p.few || p.piece < vocab ? (size_t)rows * p.pitch * 4 * p.dx.splits : 0);
         take(p.dw_slab, p.dw.splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw.splits : 0);
     }
     take(p.xcopy, (size_t)p.krows * p.pitch * 2 * p.limbs);
@@ -829,6 +903,16 @@ static hipError_t operand(const XentPlan &pl, const T *src, char *copy, int64_t 
     return launch_result();
 }
 
+// rows of more classes than one batch of 256 threads take 1024
+constexpr int XENT_WIDE = 1024 * XENT_BATCH;
+
+static hipError_t row_loss(const float *z, int splits, int rows, int ld, const int64_t *labels, float *loss, float *lse, int vocab, hipStream_t st)
+{
+    const auto kernel = vocab > XENT_WIDE ? xent_row_loss<16> : xent_row_loss<4>;
+    NGC_LAUNCH(kernel, dim3(rows), dim3(vocab > XENT_WIDE ? 1024 : 256), 0, st, z, splits, (size_t)rows * ld, ld, labels, loss, lse, vocab);
+    return launch_result();
+}
+
 template <typename T>
 static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, const T *w, const int64_t *labels, float *loss, float *lse, char *ws, hipStream_t st)
 {
@@ -847,8 +931,7 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
         float *z = reinterpret_cast<float *>(ws + pl.zslab);
         const int ld = (int)up(vocab, 8);
         if ((e = launch_few_z(p.mm.a, p.mm.alimb, pl.pitch, w, z, rows, width, vocab, st)) != hipSuccess) return e;
-        NGC_LAUNCH(xent_row_loss, dim3(rows), dim3(256), 0, st, z, 1, (size_t)0, ld, labels, loss, lse, vocab);
-        return launch_result();
+        return row_loss(z, 1, rows, ld, labels, loss, lse, vocab, st);
     }
     int tiles = 0;
     for (int64_t v0 = 0; v0 < vocab; v0 += p.mm.N) {
@@ -864,8 +947,7 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
             p.ldo = p.store_n = ld; p.store_m = rows;
             p.mm.splits = pl.z.splits;
             if ((e = launch_mm<T, false, false, XE_SLAB>(p, pl.z.edge, st)) != hipSuccess) return e;
-            NGC_LAUNCH(xent_row_loss, dim3(rows), dim3(256), 0, st, p.slab, pl.z.splits, (size_t)rows * ld, ld, labels, loss, lse, vocab);
-            return launch_result();
+            return row_loss(p.slab, pl.z.splits, rows, ld, labels, loss, lse, vocab, st);
         }
         const int edge = copy_w || pl.piece == vocab ? pl.z.edge : mm_choose(rows, vocab, pl.pitch, pl.limbs, 1, false).edge;
         if ((e = launch_mm<T, false, false, XE_STATS>(p, edge, st)) != hipSuccess) return e;
@@ -895,8 +977,8 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
     if (!pl.by_rows && (e = launch_result()) != hipSuccess) return e;
     const uint16_t *xp, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
     if ((e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
-    const bool one = pl.piece >= vocab && pl.dx.splits == 1 && !pl.few;  // dx leaves the products whole
-    const bool together = dx && dw && !pl.few && pl.dw.splits == 1 && pl.dx.edge == pl.dw.edge && pl.dw.edge < 256;
+    const bool one = pl.dx.splits == 1 && !pl.few;                       // dx leaves the products whole
+    const bool together = dx && dw && !pl.few && pl.piece >= vocab && pl.dw.splits == 1 && pl.dx.edge == pl.dw.edge && pl.dw.edge < 256;
     for (int64_t v0 = 0; v0 < vocab; v0 += pl.piece) {
         const int piece = vocab - v0 < pl.piece ? (int)(vocab - v0) : pl.piece, gp = (int)up(piece, 64);
         const int kpiece = (int)(pl.limbs == 3 ? up(piece, 32) : piece);
@@ -917,7 +999,8 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             q.mm.splits = pl.z.splits;
             e = pl.few ? launch_few_z(xp, q.mm.alimb, pl.pitch, w, q.slab, rows, width, vocab, st) : launch_mm<T, false, false, XE_SLAB>(q, pl.z.edge, st);
             if (e != hipSuccess) return e;
-            NGC_LAUNCH((xent_row_grad<T>), dim3((unsigned)pl.krows), dim3(256), 0, st, q.slab, pl.z.splits, (size_t)rows * ld, ld, labels, lse, dloss,
+            const auto kernel = vocab > XENT_WIDE ? xent_row_grad<T, 16> : xent_row_grad<T, 4>;
+            NGC_LAUNCH(kernel, dim3((unsigned)pl.krows), dim3(vocab > XENT_WIDE ? 1024 : 256), 0, st, q.slab, pl.z.splits, (size_t)rows * ld, ld, labels, lse, dloss,
                        reinterpret_cast<uint16_t *>(ws + pl.g), p.glimb, gp, scale, rows, vocab);
             e = launch_result();
         } else {
@@ -932,8 +1015,9 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             q.mm.a = g; q.mm.lda = gp; q.mm.alimb = p.glimb;
             q.mm.M = rows; q.mm.N = pl.pitch; q.mm.K = kpiece; q.mm.splits = pl.dx.splits;
             q.store_m = rows;
-            if (one) {
+            if (pl.dx.splits == 1 && v0 + piece >= vocab) {              // the last piece leaves the result
                 q.out = dx; q.ldo = width; q.store_n = width;
+                q.slab = dx_slab; q.add = v0 > 0;
                 if (!together) e = launch_mm<T, false, true, XE_OUT>(q, pl.dx.edge, st);
             } else {
                 q.slab = dx_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = v0 > 0;
@@ -943,8 +1027,10 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             both = q;
         }
         if (dw && pl.few && rows <= 16) {
-            NGC_LAUNCH((xent_few_dw<T>), dim3((unsigned)((vocab + 63) / 64), (unsigned)((width + 1023) / 1024)), dim3(256), 0, st, g, p.glimb, gp, x, scale, dw, rows,
-                       width, vocab);
+            const int lanes = width <= 64 ? 16 : width <= 256 ? 64 : 256;
+            const auto kernel = lanes == 16 ? xent_few_dw<T, 16> : lanes == 64 ? xent_few_dw<T, 64> : xent_few_dw<T, 256>;
+            NGC_LAUNCH(kernel, dim3((unsigned)((vocab + 63) / 64), (unsigned)((width + 4 * lanes - 1) / (4 * lanes))), dim3(256), 0, st, g, p.glimb, gp, x, scale, dw,
+                       rows, width, vocab);
             if ((e = launch_result()) != hipSuccess) return e;
         } else if (dw) {
             XentMm q = p;
