@@ -72,10 +72,15 @@ hipError_t launch_embedding(int dtype, int64_t tokens, int vocab, int width, flo
 //   3  chunks of the sorted tokens that belong to one id: their sums (frequent ids only: padding, articles)
 //   4  the rows that have tokens: tokens up to the first chunk, chunks, tokens behind the last, times scale
 // Both sorts rank a wave's 64 tokens among each other with one ballot per bit of the bin, and waves own consecutive tokens.
-
-constexpr int EMB_RANGES = 2048, EMB_BLOCKS = 512, EMB_TILE = 2048;
+// Up to 8192 tokens take three launches: each range looks through all tokens itself (from the L2), which costs less than a launch that sorts
+// blocks (5001 tokens, 10007 rows of 777, fp32, all launches: 31.8 -> 27 us; 2197 tokens, 23311 rows of 2209: 7 us for launch 1 alone).  Above,
+// the looking grows with tokens x ranges.
+// Bound: HBM, dy read once and dtable written once.
+constexpr int EMB_RANGES = 2048, EMB_BLOCKS = 512, EMB_TILE = 2048, EMB_SCAN = 8192;
+constexpr int EMB_MOST = 1 << 10;                        // ids of a range at most
 
 struct EmbPlan {
+    bool scan;
     int shift, ranges, blocks, chunk;
     int64_t per_block, chunks;                           // tokens of a block (a multiple of EMB_TILE)
     size_t starts, byrange, byid, rowstart, sums, total; // offsets in the workspace
@@ -84,7 +89,8 @@ struct EmbPlan {
 static EmbPlan emb_plan(int64_t tokens, int vocab, int width)
 {
     EmbPlan p{};
-    while (((vocab - 1) >> p.shift) >= EMB_RANGES) ++p.shift;
+    p.scan = tokens <= EMB_SCAN;
+    while (((vocab - 1) >> p.shift) >= (p.scan && vocab < EMB_MOST * 1024 ? 1024 : EMB_RANGES)) ++p.shift;
     p.ranges = ((vocab - 1) >> p.shift) + 1;
     p.per_block = (tokens + EMB_BLOCKS - 1) / EMB_BLOCKS;
     p.per_block = p.per_block < EMB_TILE ? EMB_TILE : (p.per_block + EMB_TILE - 1) / EMB_TILE * EMB_TILE;
@@ -93,10 +99,14 @@ static EmbPlan emb_plan(int64_t tokens, int vocab, int width)
     p.chunk = 32;
     while ((int64_t)p.chunk * p.chunk < tokens / 16 && p.chunk < 4096) p.chunk *= 2;
     p.chunks = tokens / p.chunk;
+    if (tokens < 256) {                                  // one launch less; a row of all tokens takes 32 steps
+        p.chunk = 1 << 30;
+        p.chunks = 0;
+    }
     size_t at = 0;
     auto take = [&](size_t &where, size_t bytes) { where = at; at += (bytes + 255) & ~(size_t)255; };
-    take(p.starts, (size_t)(p.ranges + 1) * p.blocks * 4);
-    take(p.byrange, (size_t)tokens * 8);
+    take(p.starts, p.scan ? 0 : (size_t)(p.ranges + 1) * p.blocks * 4);
+    take(p.byrange, p.scan ? 0 : (size_t)tokens * 8);
     take(p.byid, (size_t)tokens * 4);
     take(p.rowstart, ((size_t)vocab + 1) * 4);
     take(p.sums, (size_t)p.chunks * width * 4);
@@ -234,13 +244,88 @@ __global__ __launch_bounds__(512) void embedding_sort_blocks(const int64_t *__re
     }
 }
 
+// Second half of the sort, by a workgroup of 256: the tokens of a range, of which wave w holds entries lo .. hi - 1 (token, id within the range), all
+// waves' in the tokens' order; base: tokens of lower ids.  cnt: 4 x size words, none: size bytes, sm: 4 words of LDS.
+template <class F>
+__device__ __forceinline__ void sort_range(unsigned lo, unsigned hi, F entry, unsigned base, unsigned all, int range, bool last, int shift, unsigned *cnt, uint8_t *none,
+                                           unsigned *sm, unsigned *__restrict__ byid, unsigned *__restrict__ rowstart, float *__restrict__ dtable, int vocab, int width)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, size = 1 << shift;
+    for (int i = threadIdx.x; i < 4 * size; i += 256) cnt[i] = 0;
+    __syncthreads();
+    if (size > 1) {
+        for (unsigned e = lo + lane; e < hi; e += 256) {
+            unsigned id[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) id[k] = e + 64 * k < hi ? entry(e + 64 * k).y : 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (e + 64 * k < hi) atomicAdd(&cnt[wave * size + id[k]], 1u);
+        }
+    } else if (lane == 0) {
+        cnt[wave] = hi > lo ? hi - lo : 0;
+    }
+    __syncthreads();
+    unsigned sum = 0, total;
+    const int rows = (size + 255) / 256;                 // ids of a thread
+    for (int k = 0; k < rows; ++k) {
+        const int r = threadIdx.x * rows + k;
+        if (r < size)
+            for (int w = 0; w < 4; ++w) sum += cnt[w * size + r];
+    }
+    unsigned at = block_scan<4>(sum, sm, total);
+    for (int k = 0; k < rows; ++k) {
+        const int r = threadIdx.x * rows + k;
+        if (r >= size) break;
+        const int64_t v = ((int64_t)range << shift) + r;
+        if (v <= vocab) rowstart[v] = base + at;         // v = vocab: the end of the last row, if it falls inside the last range
+        const unsigned begin = at;
+        for (int w = 0; w < 4; ++w) {
+            const unsigned c = cnt[w * size + r];
+            cnt[w * size + r] = at;
+            at += c;
+        }
+        none[r] = at == begin && v < vocab;
+    }
+    if (last && threadIdx.x == 0) rowstart[vocab] = base + all;
+    __syncthreads();
+    for (unsigned e = lo; e < hi; e += 256) {
+        uint2 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = e + 64 * k + lane < hi ? entry(e + 64 * k + lane) : make_uint2(0, 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool live = e + 64 * k + lane < hi;
+            const unsigned to = place_in_order(cnt + wave * size, v[k].y, shift, live, lane);
+            if (live) byid[base + to] = v[k].x;
+        }
+    }
+    // Zeros of a row as whole 16 bytes of memory, wherever it begins, by as many lanes as it has of them (62700 rows of 19 columns: 28 -> 11 us
+    // against all lanes on a row).  Rows of whole 128-byte lines are streamed past the cache, which keeps dy there (16384 tokens bf16, 32000 rows
+    // of 2048, all launches: 98 -> 91 us); lines that two rows share are not (206 MB of rows of 2209: 60 us streamed, 32 us through the cache)
+    const bool lines = (width & 31) == 0 && (reinterpret_cast<uintptr_t>(dtable) & 127) == 0;
+    const int lanes = width <= 32 ? 8 : width <= 256 ? 64 : 256;
+    const uint64_t skew = (reinterpret_cast<uintptr_t>(dtable) >> 2) & 3;
+    float *const grid16 = dtable - skew;
+    for (int r = threadIdx.x / lanes; r < size; r += 256 / lanes) {
+        if (!none[r]) continue;
+        const uint64_t from = (uint64_t)(((int64_t)range << shift) + r) * width + skew, to = from + width, q0 = (from + 3) >> 2, q1 = to >> 2;
+        const int l = threadIdx.x & (lanes - 1);
+        for (uint64_t q = q0 + l; q < q1; q += lanes) store16_result(grid16 + 4 * q, make_uint4(0, 0, 0, 0), lines);
+        if (l < 8) {                                     // up to three floats in front and behind (or all of a row inside one 16 bytes)
+            const uint64_t i = l < 4 ? from + l : (q1 >= q0 ? 4 * q1 : to) + (l - 4);
+            if (l < 4 ? i < to && i < 4 * q0 : i < to) grid16[i] = 0.f;
+        }
+    }
+}
+
 __global__ __launch_bounds__(256) void embedding_sort_ranges(const uint2 *__restrict__ byrange, const unsigned *__restrict__ starts, unsigned *__restrict__ byid,
                                                              unsigned *__restrict__ rowstart, float *__restrict__ dtable, int vocab, int width, int shift, int blocks,
                                                              int64_t per_block)
 {
-    __shared__ unsigned pre[EMB_BLOCKS + 1], from[EMB_BLOCKS], cnt[4 << 10], sm[4];
-    __shared__ uint8_t none[1 << 10];                    // ids without tokens
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, range = blockIdx.x, size = 1 << shift;
+    __shared__ unsigned pre[EMB_BLOCKS + 1], from[EMB_BLOCKS], cnt[4 * EMB_MOST], sm[4];
+    __shared__ uint8_t none[EMB_MOST];
+    const int wave = threadIdx.x >> 6, range = blockIdx.x;
     unsigned base = 0, all = 0;
     // segments of this range: two blocks a thread
     unsigned s0[2], len[2];
@@ -263,8 +348,6 @@ __global__ __launch_bounds__(256) void embedding_sort_ranges(const uint2 *__rest
     }
     if (threadIdx.x == 255) pre[EMB_BLOCKS] = all;
     (void)block_scan<4>(s0[0] + s0[1], sm, base);        // base: tokens of lower ids
-    for (int i = threadIdx.x; i < 4 * size; i += 256) cnt[i] = 0;
-    __syncthreads();
     const unsigned per_wave = (all + 255) / 256 * 64, lo = wave * per_wave, hi = lo + per_wave < all ? lo + per_wave : all;
     auto entry = [&](unsigned e) {                       // the block whose segment holds entry e
         int a = 0, b = blocks;
@@ -275,65 +358,37 @@ __global__ __launch_bounds__(256) void embedding_sort_ranges(const uint2 *__rest
         }
         return byrange[a * per_block + from[a] + (e - pre[a])];
     };
-    if (size > 1) {
-        for (unsigned e = lo + lane; e < hi; e += 256) {
-            unsigned id[4];
+    sort_range(lo, hi, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
+}
+
+// SCAN: a wave looks through a quarter of the tokens, keeps those of the range in their order and counts those of lower ids
+__global__ __launch_bounds__(256) void embedding_sort_scan(const int64_t *__restrict__ ids, unsigned *__restrict__ byid, unsigned *__restrict__ rowstart,
+                                                           float *__restrict__ dtable, int tokens, int vocab, int width, int shift)
+{
+    __shared__ unsigned list[4][EMB_SCAN / 4], cnt[4 * EMB_MOST], sm[4];
+    __shared__ uint8_t none[EMB_MOST];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, range = blockIdx.x;
+    const int share = (tokens + 255) / 256 * 64, t0 = wave * share, t1 = t0 + share < tokens ? t0 + share : tokens;
+    unsigned mine = 0, lower = 0;
+    for (int t = t0; t < t1; t += 512) {
+        int64_t id[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) id[k] = e + 64 * k < hi ? entry(e + 64 * k).y : 0u;
+        for (int k = 0; k < 8; ++k) id[k] = t + 64 * k + lane < t1 ? ids[t + 64 * k + lane] : -1;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (e + 64 * k < hi) atomicAdd(&cnt[wave * size + id[k]], 1u);
-        }
-        __syncthreads();
-    } else if (lane == 0) {
-        cnt[wave] = hi > lo ? hi - lo : 0;
-    }
-    __syncthreads();
-    unsigned sum = 0, total;
-    const int rows = (size + 255) / 256;                 // ids of a thread
-    for (int k = 0; k < rows; ++k) {
-        const int r = threadIdx.x * rows + k;
-        if (r < size)
-            for (int w = 0; w < 4; ++w) sum += cnt[w * size + r];
-    }
-    at = block_scan<4>(sum, sm, total);
-    for (int k = 0; k < rows; ++k) {
-        const int r = threadIdx.x * rows + k;
-        if (r >= size) break;
-        const int64_t v = ((int64_t)range << shift) + r;
-        if (v <= vocab) rowstart[v] = base + at;         // v = vocab: the end of the last row, if it falls inside the last range
-        const unsigned begin = at;
-        for (int w = 0; w < 4; ++w) {
-            const unsigned c = cnt[w * size + r];
-            cnt[w * size + r] = at;
-            at += c;
-        }
-        none[r] = at == begin && v < vocab;
-    }
-    if (range == (int)gridDim.x - 1 && threadIdx.x == 0) rowstart[vocab] = base + all;
-    __syncthreads();
-    for (unsigned e = lo; e < hi; e += 256) {
-        uint2 v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = e + 64 * k + lane < hi ? entry(e + 64 * k + lane) : make_uint2(0, 0);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const bool live = e + 64 * k + lane < hi;
-            const unsigned to = place_in_order(cnt + wave * size, v[k].y, shift, live, lane);
-            if (live) byid[base + to] = v[k].x;
+        for (int k = 0; k < 8; ++k) {
+            const bool live = id[k] >= 0 && id[k] < vocab;
+            const int r = live ? (int)(id[k] >> shift) : -1;
+            const uint64_t here = __ballot(r == range);
+            if (r == range) list[wave][mine + __popcll(here & ((1ull << lane) - 1))] = (unsigned)(t + 64 * k + lane) << 16 | ((unsigned)id[k] & ((1u << shift) - 1));
+            mine += __popcll(here);
+            lower += __popcll(__ballot(live && r < range));
         }
     }
-    for (int r = 0; r < size; ++r) {
-        if (!none[r]) continue;
-        float *row = dtable + (size_t)(((int64_t)range << shift) + r) * width;
-        int col;
-        const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (width < 4) {
-            if (column_of<true>(threadIdx.x, width, col)) store_group<true>(row + col, zero);
-        } else {
-            for (int g = threadIdx.x; column_of<false>(g, width, col); g += 256) store_group<false>(row + col, zero);
-        }
-    }
+    unsigned base, all;
+    (void)block_scan<4>(lane == 0 ? lower : 0, sm, base);
+    (void)block_scan<4>(lane == 0 ? mine : 0, sm, all);
+    auto entry = [&](unsigned e) { return make_uint2(list[wave][e] >> 16, list[wave][e] & 0xFFFFu); };
+    sort_range(0, mine, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
 }
 
 // sum[u] += rows row(lo) .. row(hi - 1) of dy, columns col[u] ..; U groups per lane.  lo and hi are the same in all lanes.  The loads of B rows are
@@ -432,14 +487,18 @@ static hipError_t launch_embedding_bwd_t(int64_t tokens, int vocab, int width, f
     unsigned *starts = reinterpret_cast<unsigned *>(ws + p.starts), *byid = reinterpret_cast<unsigned *>(ws + p.byid), *rowstart = reinterpret_cast<unsigned *>(ws + p.rowstart);
     uint2 *byrange = reinterpret_cast<uint2 *>(ws + p.byrange);
     float *sums = reinterpret_cast<float *>(ws + p.sums);
-    int bits = 0;
-    while ((1 << bits) < p.ranges) ++bits;
-    static LdsLimitOnce lds;
-    hipError_t e = lds.raise(reinterpret_cast<const void *>(&embedding_sort_blocks));
-    if (e != hipSuccess) return e;
-    NGC_LAUNCH(embedding_sort_blocks, dim3(p.blocks), dim3(512), (p.ranges + 1) * 8 * 4, st, ids, byrange, starts, tokens, vocab, p.shift, bits, p.ranges, p.per_block);
-    if ((e = launch_result()) != hipSuccess) return e;
-    NGC_LAUNCH(embedding_sort_ranges, dim3(p.ranges), dim3(256), 0, st, byrange, starts, byid, rowstart, dtable, vocab, width, p.shift, p.blocks, p.per_block);
+    hipError_t e;
+    if (p.scan) {
+        NGC_LAUNCH(embedding_sort_scan, dim3(p.ranges), dim3(256), 0, st, ids, byid, rowstart, dtable, (int)tokens, vocab, width, p.shift);
+    } else {
+        int bits = 0;
+        while ((1 << bits) < p.ranges) ++bits;
+        static LdsLimitOnce lds;
+        if ((e = lds.raise(reinterpret_cast<const void *>(&embedding_sort_blocks))) != hipSuccess) return e;
+        NGC_LAUNCH(embedding_sort_blocks, dim3(p.blocks), dim3(512), (p.ranges + 1) * 8 * 4, st, ids, byrange, starts, tokens, vocab, p.shift, bits, p.ranges, p.per_block);
+        if ((e = launch_result()) != hipSuccess) return e;
+        NGC_LAUNCH(embedding_sort_ranges, dim3(p.ranges), dim3(256), 0, st, byrange, starts, byid, rowstart, dtable, vocab, width, p.shift, p.blocks, p.per_block);
+    }
     if ((e = launch_result()) != hipSuccess) return e;
     const int groups = width < 4 ? width : width / 4 + (width % 4 != 0);
     if (p.chunks) {
