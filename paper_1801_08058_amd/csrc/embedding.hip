@@ -73,7 +73,7 @@ hipError_t launch_embedding(int dtype, int64_t tokens, int vocab, int width, flo
 //   4  the rows that have tokens: tokens up to the first chunk, chunks, tokens behind the last, times scale
 // Both sorts rank a wave's 64 tokens among each other with one ballot per bit of the bin, and waves own consecutive tokens.
 // Up to 8192 tokens take three launches: each range looks through all tokens itself (from the L2), which costs less than a launch that sorts
-// blocks (5001 tokens, 10007 rows of 777, fp32, all launches: 31.8 -> 27 us; 2197 tokens, 23311 rows of 2209: 7 us for launch 1 alone).  Above,
+// blocks (5001 tokens, 10007 rows of 777, fp32, all launches: 31.8 -> 27 us; 18935 tokens: 7.6 us for launch 1 alone).  Above,
 // the looking grows with tokens x ranges.
 // Bound: HBM, dy read once and dtable written once.
 constexpr int EMB_RANGES = 2048, EMB_BLOCKS = 512, EMB_TILE = 2048, EMB_SCAN = 8192;

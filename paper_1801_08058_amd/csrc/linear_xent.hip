@@ -23,41 +23,68 @@ struct XentRow {
     int label, pad;
 };
 
-// One workgroup.  The gradient's rows are scaled by dloss / max |dloss| before they are rounded to bf16, and the results by max |dloss| in
-// fp32: where all rows weigh the same (a mean), the weight's own rounding would otherwise be the same in every term of the sums.
-__global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ labels, const float *__restrict__ lse, const float *__restrict__ dloss,
-                                                  XentRow *__restrict__ info, float *__restrict__ scale, int rows, int vocab)
-{
-    __shared__ float sm[16];
-    constexpr int B = 8;                                                 // rows of a thread whose loads are under way together
-    int64_t label[B];
-    float weight[B], l[B], top = 0.f;
-    auto load = [&](int m0) {
+constexpr int XENT_ROWS = 8192, XENT_TOPS = 256;         // rows of a workgroup's step; workgroups at most
+
+// What a workgroup of 1024 takes of XENT_ROWS rows from m0 on: eight rows a thread, whose loads are under way together
+struct XentRows {
+    static constexpr int B = XENT_ROWS / 1024;
+    int64_t label[B];                                                    // -1: does not count
+    float weight[B], l[B];
+    __device__ __forceinline__ void load(const int64_t *labels, const float *dloss, const float *lse, int64_t m0, int rows, int vocab)
+    {
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-            const int m = m0 + 1024 * b + threadIdx.x;
+            const int64_t m = m0 + 1024 * b + threadIdx.x;
             label[b] = -1;
-            if (m < rows) label[b] = labels[m], weight[b] = dloss[m], l[b] = lse[m];
+            if (m < rows) label[b] = labels[m], weight[b] = dloss[m], l[b] = lse ? lse[m] : 0.f;
             if (label[b] >= vocab) label[b] = -1;
         }
-    };
-    for (int m0 = 0; m0 < rows; m0 += 1024 * B) {
-        load(m0);
+    }
+    __device__ __forceinline__ float most(float top) const
+    {
 #pragma unroll
         for (int b = 0; b < B; ++b)
             if (label[b] >= 0) top = fmaxf(top, fabsf(weight[b]));
+        return top;
     }
+};
+
+// Largest |dloss| of the rows that count, workgroup by workgroup: where one workgroup does not take all rows in a step
+__global__ __launch_bounds__(1024) void xent_tops(const int64_t *__restrict__ labels, const float *__restrict__ dloss, float *__restrict__ tops, int rows, int vocab)
+{
+    __shared__ float sm[16];
+    XentRows r;
+    float top = 0.f;
+    for (int64_t m0 = (int64_t)blockIdx.x * XENT_ROWS; m0 < rows; m0 += (int64_t)gridDim.x * XENT_ROWS) {
+        r.load(labels, dloss, nullptr, m0, rows, vocab);
+        top = r.most(top);
+    }
+    top = block_reduce<16>(top, true, sm);
+    if (threadIdx.x == 0) tops[blockIdx.x] = top;
+}
+
+// The gradient's rows are scaled by dloss / max |dloss| before they are rounded to bf16, and the results by max |dloss| in fp32: where all rows
+// weigh the same (a mean), the weight's own rounding would otherwise be the same in every term of the sums.  count: the workgroups that left tops;
+// 0: the only workgroup sees all rows.  (65536 rows: 38 us by one workgroup, 11 us in two launches of eight.)
+__global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ labels, const float *__restrict__ lse, const float *__restrict__ dloss,
+                                                  const float *__restrict__ tops, int count, XentRow *__restrict__ info, float *__restrict__ scale, int rows, int vocab)
+{
+    __shared__ float sm[16];
+    XentRows r;
+    r.load(labels, dloss, lse, (int64_t)blockIdx.x * XENT_ROWS, rows, vocab);
+    float top = count ? ((int)threadIdx.x < count ? tops[threadIdx.x] : 0.f) : r.most(0.f);
     top = fmaxf(block_reduce<16>(top, true, sm), 0x1p-100f);             // all zero: any scale
     const float inv = 1.0f / top;
-    for (int m0 = 0; m0 < rows; m0 += 1024 * B) {
-        if (rows > 1024 * B) load(m0);
+    for (int64_t m0 = (int64_t)blockIdx.x * XENT_ROWS; m0 < rows;) {
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const int m = m0 + 1024 * b + threadIdx.x;
-            if (m < rows) info[m] = XentRow{l[b] * LOG2E, label[b] >= 0 ? weight[b] * inv : 0.f, label[b] >= 0 ? (int)label[b] : -1, 0};
+        for (int b = 0; b < XentRows::B; ++b) {
+            const int64_t m = m0 + 1024 * b + threadIdx.x;
+            if (m < rows) info[m] = XentRow{r.l[b] * LOG2E, r.label[b] >= 0 ? r.weight[b] * inv : 0.f, r.label[b] >= 0 ? (int)r.label[b] : -1, 0};
         }
+        m0 += (int64_t)gridDim.x * XENT_ROWS;
+        if (m0 < rows) r.load(labels, dloss, lse, m0, rows, vocab);
     }
-    if (threadIdx.x == 0) *scale = top;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *scale = top;
 }
 
 // Eight values as L limbs: the value rounded to bf16, what that leaves, rounded, and what that leaves (one limb: values that bf16 holds)
@@ -98,7 +125,7 @@ enum XentEpilogue { XE_STATS, XE_GRAD, XE_SLAB, XE_OUT };
 
 struct XentMm {
     MmParams mm;
-    int v0, vocab;                       // STATS, GRAD: first class of the piece, classes in all
+    int v0;                              // STATS, GRAD: first class of the piece
     const int64_t *labels;               // STATS
     float2 *part;                        // STATS: [tiles][rows], from this piece's first tile on
     float *target;                       // STATS
@@ -762,7 +789,7 @@ struct XentPlan {
     MmChoice z, dx, dw;          // products of a whole piece
     bool by_rows;                // z in slabs, then a workgroup per row
     bool few;                    // by_rows with the weight straight from memory; dx as well, in dx.splits parts
-    size_t info, scale, zslab, xcopy, wcopy, g, dx_slab, dw_slab, total; // offsets in the workspace
+    size_t info, scale, tops, zslab, xcopy, wcopy, g, dx_slab, dw_slab, total; // offsets in the workspace
 };
 
 static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
@@ -820,6 +847,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
     } else {
         take(p.info, (size_t)rows * sizeof(XentRow));
         take(p.scale, 4);
+        take(p.tops, rows > XENT_ROWS ? XENT_TOPS * 4 : 0);
         take(p.g, (size_t)p.krows * up(p.piece, 64) * 2 * p.limbs);
         take(p.dx_slab, p.dx.splits > 1 || p.few || p.piece < vocab ? (size_t)rows * p.pitch * 4 * p.dx.splits : 0);
         take(p.dw_slab, p.dw.splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw.splits : 0);
@@ -924,7 +952,7 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
     p.mm.lda = p.mm.ldb = pl.pitch;
     p.mm.M = rows; p.mm.K = pl.pitch; p.mm.splits = 1;
     p.mm.alimb = (int64_t)rows * pl.pitch;
-    p.vocab = vocab; p.labels = labels;
+    p.labels = labels;
     p.target = reinterpret_cast<float *>(ws + pl.scale);
     float2 *part = reinterpret_cast<float2 *>(ws + pl.info);
     if (pl.few) {
@@ -973,8 +1001,16 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
     XentRow *info = reinterpret_cast<XentRow *>(ws + pl.info);
     float *scale = reinterpret_cast<float *>(ws + pl.scale), *dx_slab = reinterpret_cast<float *>(ws + pl.dx_slab), *dw_slab = reinterpret_cast<float *>(ws + pl.dw_slab);
     hipError_t e = hipSuccess;
-    if (!pl.by_rows) NGC_LAUNCH(xent_rows, dim3(1), dim3(1024), 0, st, labels, lse, dloss, info, scale, rows, vocab);
-    if (!pl.by_rows && (e = launch_result()) != hipSuccess) return e;
+    if (!pl.by_rows) {
+        const int need = (rows - 1) / XENT_ROWS + 1, grid = need < XENT_TOPS ? need : XENT_TOPS;
+        float *tops = reinterpret_cast<float *>(ws + pl.tops);
+        if (grid > 1) {
+            NGC_LAUNCH(xent_tops, dim3(grid), dim3(1024), 0, st, labels, dloss, tops, rows, vocab);
+            if ((e = launch_result()) != hipSuccess) return e;
+        }
+        NGC_LAUNCH(xent_rows, dim3(grid), dim3(1024), 0, st, labels, lse, dloss, tops, grid > 1 ? grid : 0, info, scale, rows, vocab);
+        if ((e = launch_result()) != hipSuccess) return e;
+    }
     const uint16_t *xp, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
     if ((e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
     const bool one = pl.dx.splits == 1 && !pl.few;                       // dx leaves the products whole
@@ -985,7 +1021,7 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
         if (pl.few) wp = nullptr;                                        // w is read where it is
         else if ((e = operand(pl, w + (size_t)v0 * width, ws + pl.wcopy, piece, kpiece, width, wp, st)) != hipSuccess) return e;
         XentMm p{};
-        p.v0 = (int)v0; p.vocab = vocab; p.info = info; p.scale = scale;
+        p.v0 = (int)v0; p.info = info; p.scale = scale;
         p.mm.a = xp; p.mm.b = wp;
         p.mm.lda = p.mm.ldb = pl.pitch;
         p.mm.alimb = pl.krows * pl.pitch; p.mm.blimb = (int64_t)kpiece * pl.pitch;

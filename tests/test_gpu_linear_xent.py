@@ -179,3 +179,33 @@ def test_few_rows_over_many_classes(dtype, rows, width, vocab):
     print(f"linear_xent few {rows} {width} {vocab} {dtype}", flush=True)
     _check(dtype, *_inputs(dtype, rows, width, vocab, 81 + rows))
     _check(dtype, *_inputs(dtype, rows, width, vocab, 82 + rows), offset=1)
+
+
+# more rows than one workgroup looks at in a step for the largest weight
+@pytest.mark.parametrize("dtype,rows,width,vocab", [("bf16", 8192, 16, 40), ("bf16", 8193, 24, 40), ("f32", 20001, 20, 33)])
+def test_many_rows(dtype, rows, width, vocab):
+    print(f"linear_xent many {rows} {width} {vocab} {dtype}", flush=True)
+    x, w, labels, dloss = _inputs(dtype, rows, width, vocab, 91 + rows)
+    labels[-1], dloss[-1] = vocab // 2, 50.0                 # the largest weight in the last row
+    _check(dtype, x, w, labels, dloss)
+
+
+@pytest.mark.parametrize("rows,vocab", [(60, 500), (600, 9000), (17000, 40)])
+def test_weights_of_rows_that_do_not_count(rows, vocab):
+    x, w, labels, dloss = _inputs("bf16", rows, 32, vocab, 95 + rows)
+    labels[::7] = -1
+    dead = (labels < 0) | (labels >= vocab)
+    dev = lambda a, t: torch.from_numpy(np.ascontiguousarray(a)).to(t).cuda()
+    xd, wd, ld = dev(x, torch.bfloat16), dev(w, torch.bfloat16), dev(labels, torch.int64)
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    ws = torch.empty(max(ng.ngc_linear_xent_workspace_bytes(ng.NGC_BF16, rows, 32, vocab, b) for b in (0, 1)), dtype=torch.uint8, device="cuda")
+    ng.ngc_linear_xent(ng.NGC_BF16, rows, 32, vocab, xd, wd, ld, loss, lse, ws, stream())
+    got = []
+    for weight in (0.0, 3e38):
+        dx, dw = torch.empty_like(xd), torch.empty_like(wd)
+        gd = dev(np.where(dead, np.float32(weight), dloss), torch.float32)
+        ng.ngc_linear_xent_bwd(ng.NGC_BF16, rows, 32, vocab, xd, wd, ld, lse, gd, dx, dw, ws, stream())
+        torch.cuda.synchronize()
+        got.append((dx, dw))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert bool((got[0][0][torch.from_numpy(dead).cuda()] == 0).all())
