@@ -434,22 +434,30 @@ __global__ __launch_bounds__(64 * NW) void xent_row_grad(const float *__restrict
 // ---- few rows, and a weight that the products above would have to copy (fp32, rows of no multiple of 16 bytes) ----
 //
 // The weight goes straight from memory to registers, at any alignment, and becomes limbs there: it is read once per product, where a copy
-// reads it, writes three bf16 values per element and reads those.  Bound: HBM.
+// reads it, writes three bf16 values per element and reads those.  Bound: HBM (fp32, 33024 classes of 1024: 27 us for 8 rows, 5.0 TB/s, 47 for 64);
+// bf16 rows of odd lengths the L1, which serves loads off the 4-byte grid in pieces (54005 classes of 2541, 18 rows: 108 us, fp32 143).
 
-// Eight elements of a row, `left` of them inside it (the others are zero)
+// The k of element e of lane group g within a step of 32: a lane's 16 bytes, and with them 64 bytes of a row in one load, lie together
+template <typename T> __host__ __device__ constexpr int few_k(int g, int e) { return sizeof(T) == 4 ? 16 * (e / 4) + 4 * g + e % 4 : 8 * g + e; }
+
+// A lane's eight elements of a step of a row, `left` elements of which are from the step on (those behind the row are zeros)
 template <typename T>
 struct Eight {
     uint32_t w[2 * sizeof(T)];
-    __device__ __forceinline__ void load(const T *p, int left)
+    __device__ __forceinline__ void load(const T *step, int g, int left)
     {
-        if (left >= 8) {
-            __builtin_memcpy(w, p, sizeof(w));
-            return;
-        }
+        constexpr int E = 16 / sizeof(T);                                        // elements of a load
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if constexpr (sizeof(T) == 4) w[k] = k < left ? __float_as_uint(p[k]) : 0u;
-            else if (k % 2 == 0) w[k / 2] = (k < left ? (uint32_t)p[k] : 0u) | (k + 1 < left ? (uint32_t)p[k + 1] << 16 : 0u);
+        for (int e = 0; e < 8; e += E) {
+            const int k = few_k<T>(g, e);
+            T v[E];
+            if (k + E <= left) {
+                __builtin_memcpy(v, step + k, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[i] = k + i < left ? step[k + i] : T(0);
+            }
+            __builtin_memcpy(w + e * sizeof(T) / 4, v, 16);
         }
     }
     template <int L> __device__ __forceinline__ void limbs(mm_bf16x8 (&out)[L]) const
@@ -464,72 +472,100 @@ struct Eight {
     }
 };
 
-// z[m][v] of a wave's 32 classes and MT blocks of 16 rows.  x: copied, limbs xlimb elements apart
-template <typename T, int MT>
-__global__ __launch_bounds__(256) void xent_few_z(const uint16_t *__restrict__ x, int64_t xlimb, int pitch, const T *__restrict__ w, float *__restrict__ z, int ld,
-                                                  int rows, int width, int vocab)
+// blocks of 16 classes of a workgroup: more rows of x, which every workgroup reads, more classes for them
+constexpr int xent_few_blocks(int mt) { return mt == 1 ? 2 : 4; }
+
+// x for xent_few_z: of every step, block of 16 rows and limb what the 64 lanes hold, 1 KB in their order: eight lines a load, where rows are sixteen
+template <typename T>
+__global__ __launch_bounds__(256) void xent_pack(const T *__restrict__ x, uint4 *__restrict__ dst, int rows, int width, int blocks)
 {
     constexpr int L = sizeof(T) == 4 ? 3 : 1;
-    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
-    const int v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 32;
-    if (v0 >= vocab) return;
-    const T *row[2];
+    const int lane = threadIdx.x & 63, g = lane >> 4, n = blockIdx.x;
+    for (int j = threadIdx.x >> 6; j < blocks; j += 4) {
+        const int m = 16 * j + (lane & 15);
+        float f[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) row[i] = w + (size_t)(v0 + 16 * i + l < vocab ? v0 + 16 * i + l : vocab - 1) * width;
-    const uint16_t *xr[MT];
+        for (int e = 0; e < 8; ++e) {
+            const int k = 32 * n + few_k<T>(g, e);
+            f[e] = m < rows && k < width ? SmElem<T>::load(x + (size_t)m * width + k) : 0.f;
+        }
+        mm_bf16x8 limb[L];
+        split_limbs(f, limb);
 #pragma unroll
-    for (int j = 0; j < MT; ++j) xr[j] = x + (size_t)(16 * j + l < rows ? 16 * j + l : rows - 1) * pitch;
-    mm_f32x4 acc[2][MT];
+        for (int q = 0; q < L; ++q) dst[(((size_t)n * blocks + j) * L + q) * 64 + lane] = __builtin_bit_cast(uint4, limb[q]);
+    }
+}
+
+// z[m][v] of 16 IB classes and MT blocks of 16 rows.  The four waves take every fourth step of 32 elements and are added up through LDS: what the
+// workgroup has under way of a class lies together (fp32, 54005 classes of 2541, 18 rows: 205 us with 32 classes of its own for each wave, 143).
+// One step ahead and as many waves as fit: four steps ahead in a wave take the registers of the others, and no less time.
+template <typename T, int MT>
+__global__ __launch_bounds__(256) void xent_few_z(const uint4 *__restrict__ x, const T *__restrict__ w, float *__restrict__ z, int ld, int rows, int width,
+                                                  int vocab)
+{
+    constexpr int L = sizeof(T) == 4 ? 3 : 1, IB = xent_few_blocks(MT);
+    __shared__ mm_f32x4 sums[3][IB * MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4, v0 = blockIdx.x * 16 * IB, j0 = blockIdx.y * MT, blocks = gridDim.y * MT;
+    const T *row[IB];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < IB; ++i) row[i] = w + (size_t)(v0 + 16 * i + l < vocab ? v0 + 16 * i + l : vocab - 1) * width;
+    mm_f32x4 acc[IB][MT];
+#pragma unroll
+    for (int i = 0; i < IB; ++i)
 #pragma unroll
         for (int j = 0; j < MT; ++j) acc[i][j] = mm_f32x4{0.f, 0.f, 0.f, 0.f};
-    auto products = [&](const Eight<T> (&raw)[2], int k) {
-        mm_bf16x8 a[2][L], b[MT][L];
+    // x is under way as far ahead as the weight: loads arrive in their order, and a step that asked for its x itself would wait for the next weights
+    struct Step {
+        Eight<T> w[IB];
+        uint4 x[MT][L];
+    };
+    const int full = (width / 32 - wave + 3) / 4;                                // whole steps of this wave: wave, wave + 4, ..
+    auto load = [&](Step &to, int n, int left) {
+#pragma unroll
+        for (int i = 0; i < IB; ++i) to.w[i].load(row[i] + 32 * n, g, left);
 #pragma unroll
         for (int j = 0; j < MT; ++j)
 #pragma unroll
-            for (int q = 0; q < L; ++q) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (k < pitch) v = *reinterpret_cast<const uint4 *>(xr[j] + q * xlimb + k);             // zeros behind the row up to pitch
-                b[j][q] = __builtin_bit_cast(mm_bf16x8, v);
-            }
+            for (int q = 0; q < L; ++q) to.x[j][q] = x[(((size_t)n * blocks + j0 + j) * L + q) * 64 + lane];
+    };
+    auto products = [&](const Step &from) {
+        mm_bf16x8 a[IB][L], b[MT][L];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) raw[i].template limbs<L>(a[i]);
+        for (int j = 0; j < MT; ++j)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int q = 0; q < L; ++q) b[j][q] = __builtin_bit_cast(mm_bf16x8, from.x[j][q]);
+#pragma unroll
+        for (int i = 0; i < IB; ++i) from.w[i].template limbs<L>(a[i]);
+#pragma unroll
+        for (int i = 0; i < IB; ++i)
 #pragma unroll
             for (int j = 0; j < MT; ++j) acc[i][j] = limb_products(a[i], b[j], acc[i][j]);
     };
-    // four steps of 32 elements under way at a time
-    constexpr int AHEAD = 4;
-    const int full = width / 32;
-    Eight<T> raw[AHEAD][2];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-        if (u < full)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) raw[u][i].load(row[i] + 32 * u + 8 * g, 8);
-    for (int n = 0; n < full; n += AHEAD)
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            if (n + u >= full) break;
-            products(raw[u], 32 * (n + u) + 8 * g);
-            if (n + u + AHEAD < full)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) raw[u][i].load(row[i] + 32 * (n + u + AHEAD) + 8 * g, 8);
-        }
-    if (width % 32) {
-        const int k = 32 * full + 8 * g;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) raw[0][i].load(row[i] + (k < width ? k : 0), k < width ? width - k : 0);     // lanes past the row read nothing
-        products(raw[0], k);
+    Step now, next;
+    if (full > 0) load(next, wave, 32);
+    for (int n = 0; n < full; ++n) {
+        now = next;
+        if (n + 1 < full) load(next, 4 * (n + 1) + wave, 32);
+        products(now);
     }
+    if (width % 32 && wave == (width / 32 & 3)) {
+        load(now, width / 32, width % 32);
+        products(now);
+    }
+    if (wave)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int q = 0; q < IB * MT; ++q) sums[wave - 1][q][lane] = acc[q / MT][q % MT];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int q = 0; q < IB * MT; ++q) acc[q / MT][q % MT] += sums[s][q][lane];
+#pragma unroll
+    for (int i = 0; i < IB; ++i)
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
-            const int m = 16 * j + l, v = v0 + 16 * i + 4 * g;
+            const int m = 16 * (j0 + j) + l, v = v0 + 16 * i + 4 * g;
             if (m < rows && v < ld) *reinterpret_cast<mm_f32x4 *>(z + (size_t)m * ld + v) = acc[i][j];
         }
 }
@@ -543,7 +579,7 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
     constexpr int L = sizeof(T) == 4 ? 3 : 1;
     __shared__ mm_f32x4 sums[3][4 * MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
-    const int d = blockIdx.x * 64 + 4 * l, end = per_part * (blockIdx.y + 1) < vocab ? per_part * (blockIdx.y + 1) : vocab;
+    const int d = blockIdx.x * 64 + 4 * l, m0 = blockIdx.z * 16 * MT, end = per_part * (blockIdx.y + 1) < vocab ? per_part * (blockIdx.y + 1) : vocab;
     mm_f32x4 acc[4][MT];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -551,58 +587,88 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
         for (int j = 0; j < MT; ++j) acc[c][j] = mm_f32x4{0.f, 0.f, 0.f, 0.f};
     const uint16_t *xr[MT];
 #pragma unroll
-    for (int j = 0; j < MT; ++j) xr[j] = gr + (size_t)(16 * j + l < rows ? 16 * j + l : rows - 1) * gp;
-    struct Block {
-        float4 q[8];
+    for (int j = 0; j < MT; ++j) xr[j] = gr + (size_t)(m0 + 16 * j + l < rows ? m0 + 16 * j + l : rows - 1) * gp;
+    // A step is 32 classes, of which a lane holds four columns of eight.  A lane whose four columns end behind the row loads the row's last four, of
+    // which the products take what is theirs (shift).  fp32: one step ahead (a ring of two, unrolled, takes 216 registers instead of 160: 187 against
+    // 131 us for 54005 classes of 2541); bf16 steps are half as long, three ahead and g with them (146 -> 80 us).
+    struct Step {
+        uint32_t w[8][sizeof(T)];                                                // four elements
+        uint4 g[L == 1 ? MT : 1];
     };
-    // A lane whose four columns end behind the row loads the row's last four, of which the later products take what is theirs (shift); all loads of
-    // a block are under way together
     const int from = d + 4 <= width ? d : width - 4, shift = d - from;
-    auto load = [&](Block &blk, int v0) {
+    auto load = [&](Step &to, int v0) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int v = v0 + 8 * g + k < vocab ? v0 + 8 * g + k : vocab - 1;                          // g is zero past the classes
             const T *p = w + (size_t)v * width;
             if (width >= 4) {
-                blk.q[k] = load4_any(p + from);
+                __builtin_memcpy(to.w[k], p + from, 4 * sizeof(T));
             } else {
-                blk.q[k] = make_float4(SmElem<T>::load(p), width > 1 ? SmElem<T>::load(p + 1) : 0.f, width > 2 ? SmElem<T>::load(p + 2) : 0.f, 0.f);
+                T e[4] = {p[0], width > 1 ? p[1] : T(0), width > 2 ? p[2] : T(0), T(0)};
+                __builtin_memcpy(to.w[k], e, sizeof(e));
             }
         }
+        if constexpr (L == 1)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) to.g[j] = *reinterpret_cast<const uint4 *>(xr[j] + v0 + 8 * g);
     };
-    const bool edge = width < 4 ? l != 0 : shift != 0;
-    auto own_columns = [&](Block &blk) {
-        if (!__any(edge)) return;
+    const bool edge = width < 4 ? l != 0 : shift != 0, edges = __any(edge);
+    auto products = [&](const Step &now, int v0) {
+        float4 e[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float4 q = blk.q[k];
-            if (!edge) continue;
-            blk.q[k] = width < 4 || shift > 3 ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                              : make_float4(shift == 1 ? q.y : shift == 2 ? q.z : q.w, shift == 1 ? q.z : shift == 2 ? q.w : 0.f, shift == 1 ? q.w : 0.f, 0.f);
+            if constexpr (sizeof(T) == 4) __builtin_memcpy(&e[k], now.w[k], 16);
+            else e[k] = make_float4(__uint_as_float(now.w[k][0] << 16), __uint_as_float(now.w[k][0] & 0xFFFF0000u), __uint_as_float(now.w[k][1] << 16), __uint_as_float(now.w[k][1] & 0xFFFF0000u));
         }
-    };
-    const int begin = per_part * blockIdx.y + 32 * wave;
-    Block now, next;
-    if (begin < end) load(next, begin);
-    for (int v0 = begin; v0 < end; v0 += 128) {
-        now = next;
-        if (v0 + 128 < end) load(next, v0 + 128);
-        own_columns(now);
+        if (edges)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float4 q = e[k];
+                if (!edge) continue;
+                e[k] = width < 4 || shift > 3 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                              : make_float4(shift == 1 ? q.y : shift == 2 ? q.z : q.w, shift == 1 ? q.z : shift == 2 ? q.w : 0.f, shift == 1 ? q.w : 0.f, 0.f);
+            }
         mm_bf16x8 b[MT][L];
 #pragma unroll
         for (int j = 0; j < MT; ++j)
 #pragma unroll
-            for (int q = 0; q < L; ++q) b[j][q] = *reinterpret_cast<const mm_bf16x8 *>(xr[j] + q * glimb + v0 + 8 * g);
+            for (int q = 0; q < L; ++q)
+                if constexpr (L == 1) b[j][q] = __builtin_bit_cast(mm_bf16x8, now.g[j]);
+                else b[j][q] = *reinterpret_cast<const mm_bf16x8 *>(xr[j] + q * glimb + v0 + 8 * g);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             float f[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = c == 0 ? now.q[k].x : c == 1 ? now.q[k].y : c == 2 ? now.q[k].z : now.q[k].w;
+            for (int k = 0; k < 8; ++k) f[k] = c == 0 ? e[k].x : c == 1 ? e[k].y : c == 2 ? e[k].z : e[k].w;
             mm_bf16x8 a[L];
             split_limbs(f, a);
 #pragma unroll
             for (int j = 0; j < MT; ++j) acc[c][j] = limb_products(a, b[j], acc[c][j]);
         }
+    };
+    const int begin = per_part * blockIdx.y + 32 * wave;
+    if constexpr (L == 3) {
+        Step now, next;
+        if (begin < end) load(next, begin);
+        for (int v0 = begin; v0 < end; v0 += 128) {
+            now = next;
+            if (v0 + 128 < end) load(next, v0 + 128);
+            products(now, v0);
+        }
+    } else {
+        constexpr int NB = 4;
+        const int steps = begin < end ? (end - begin + 127) / 128 : 0;
+        Step step[NB];
+#pragma unroll
+        for (int u = 0; u < NB - 1; ++u)
+            if (u < steps) load(step[u], begin + 128 * u);
+        for (int n = 0; n < steps; n += NB)
+#pragma unroll
+            for (int u = 0; u < NB; ++u) {
+                if (n + u >= steps) break;
+                if (n + u + NB - 1 < steps) load(step[(u + NB - 1) % NB], begin + 128 * (n + u + NB - 1));
+                products(step[u], begin + 128 * (n + u));
+            }
     }
     if (wave)
 #pragma unroll
@@ -618,22 +684,23 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
     for (int j = 0; j < MT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int m = 16 * j + l, at = blockIdx.x * 64 + 16 * g + 4 * e;
+            const int m = m0 + 16 * j + l, at = blockIdx.x * 64 + 16 * g + 4 * e;
             if (m < rows && at < pitch) *reinterpret_cast<mm_f32x4 *>(out + (size_t)m * pitch + at) = mm_f32x4{acc[0][j][e], acc[1][j][e], acc[2][j][e], acc[3][j][e]};
         }
 }
 
-// dw[v][d] = scale sum_m g[m][v] x[m][d] of at most 16 rows: a thread keeps four columns of x and stores them for class after class.  A workgroup
-// takes 64 classes, their g in LDS, and 4 LPR columns; 256 / LPR classes at a time.
-template <typename T, int LPR>
+// dw[v][d] = scale sum_m g[m][v] x[m][d] of at most R rows: a thread keeps four columns of x and stores them for class after class.  A workgroup
+// takes 64 classes, their g in LDS, and 4 LPR columns; 256 / LPR classes at a time.  Bound: HBM for 16 rows, with 32 the vector instructions (fp32,
+// 54005 x 2541: 187 us, the matrix cores' tile 208; bf16 184 and 114, so 16 at most).
+template <typename T, int R, int LPR>
 __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ gr, int64_t glimb, int gp, const T *__restrict__ x, const float *__restrict__ scale,
                                                    T *__restrict__ dw, int rows, int width, int vocab)
 {
     constexpr int CLASSES = 64;
-    __shared__ float gs[CLASSES][16];
+    __shared__ float gs[CLASSES][R];
     const int v0 = blockIdx.x * CLASSES, d = (blockIdx.y * LPR + (threadIdx.x & (LPR - 1))) * 4;
     const float sc = *scale;
-    for (int i = threadIdx.x; i < CLASSES * 16; i += 256) {
+    for (int i = threadIdx.x; i < CLASSES * R; i += 256) {
         const int v = i % CLASSES, m = i / CLASSES;
         float s = 0.f;
         if (m < rows)
@@ -641,9 +708,9 @@ __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ 
             for (int q = (sizeof(T) == 4 ? 3 : 1) - 1; q >= 0; --q) s += bf16_bits_to_float(gr[q * glimb + (size_t)m * gp + v0 + v]);        // gp is a multiple of 64
         gs[v][m] = s * sc;
     }
-    float4 f[16];
+    float4 f[R];
 #pragma unroll
-    for (int m = 0; m < 16; ++m) {
+    for (int m = 0; m < R; ++m) {
         const T *p = x + (size_t)(m < rows ? m : 0) * width;
         auto at = [&](int c) { return m < rows && c < width ? SmElem<T>::load(p + c) : 0.f; };
         if (d + 4 <= width && m < rows) f[m] = load4_any(p + d);
@@ -655,7 +722,7 @@ __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ 
     for (int v = threadIdx.x / LPR; v < end; v += 256 / LPR) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int m = 0; m < 16; ++m) {
+        for (int m = 0; m < R; ++m) {
             const float g = gs[v][m];
             s.x = fmaf(g, f[m].x, s.x), s.y = fmaf(g, f[m].y, s.y), s.z = fmaf(g, f[m].z, s.z), s.w = fmaf(g, f[m].w, s.w);
         }
@@ -789,16 +856,20 @@ struct XentPlan {
     MmChoice z, dx, dw;          // products of a whole piece
     bool by_rows;                // z in slabs, then a workgroup per row
     bool few;                    // by_rows with the weight straight from memory; dx as well, in dx.splits parts
-    size_t info, scale, tops, zslab, xcopy, wcopy, g, dx_slab, dw_slab, total; // offsets in the workspace
+    bool few_dw;                 // and dw without a copy of x
+    size_t info, scale, tops, zslab, xpack, xcopy, wcopy, g, dx_slab, dw_slab, total; // offsets in the workspace
 };
 
 static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
 
-// Rows that the kernels for few rows take, 16, 32 or 64 a workgroup; more would read the weight again
-// (107 x 1921 over 33171 classes bf16: 189 us against 128 with copies).  Fewer than 8192 classes are fewer than 256 waves, and their copy is short
-// (128 x 2048 over 1000 classes fp32: 121 against 25 us).
-constexpr int XENT_FEW = 64, XENT_FEW_VOCAB = 8192;
-static int few_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+// Rows that the kernels for few rows take, 16, 32 or (fp32) 64 a workgroup; fp32 in two groups, which read the weight again.  Loss and gradients over
+// 33171 classes of 1921, with copies and without: bf16 292 -> 226 us for 1 row, 308 -> 299 for 30, 317 -> 325 for 40; fp32 716 -> 328 for 30,
+// 796 -> 432 for 60, and 495 -> 384 for 100 rows over 33000 of 1000.  Fewer than 8192 classes are fewer than 256 waves, and their copy is short
+// (128 x 2048 over 1000 classes fp32: 121 us without, 25 with copies).
+constexpr int XENT_FEW_VOCAB = 8192;
+static int few_rows(int limbs) { return limbs == 3 ? 128 : 32; }
+static int few_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }       // blocks of 16 rows of a workgroup
+static int few_groups(int64_t rows) { return (int)((rows + 63) / 64); }                  // workgroups for all rows
 
 static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bwd)
 {
@@ -827,13 +898,14 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         p.by_rows = parts.us < p.z.us && (int64_t)rows * up(vocab, 8) * 4 * parts.splits <= (32 << 20);
         if (p.by_rows) p.z = parts;
     }
-    if (p.copy && rows <= XENT_FEW && vocab >= XENT_FEW_VOCAB && (int64_t)rows * up(vocab, 8) * 4 <= (64 << 20) && vocab <= (1 << 21)) {
+    if (p.copy && rows <= few_rows(p.limbs) && vocab >= XENT_FEW_VOCAB && (int64_t)rows * up(vocab, 8) * 4 <= (64 << 20) && vocab <= (1 << 21)) {
         p.few = p.by_rows = true;
+        p.few_dw = rows <= (p.limbs == 3 ? 32 : 16);
         p.piece = vocab;
         p.z = {64, 1, 0.f};
-        // about 1024 workgroups, parts of at least 512 classes
+        // about two workgroups per compute unit, parts of at least 512 classes
         const int blocks = (int)((width + 63) / 64), most = (int)((vocab + 511) / 512);
-        p.dx = {64, 1024 / blocks < 1 ? 1 : 1024 / blocks, 0.f};
+        p.dx = {64, 512 / blocks < 1 ? 1 : 512 / blocks, 0.f};
         if (p.dx.splits > most) p.dx.splits = most;
         if (p.dx.splits > 64) p.dx.splits = 64;
         if (bwd) p.dw = mm_choose(vocab, p.pitch, rows, p.limbs, 1, false);
@@ -852,7 +924,8 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         take(p.dx_slab, p.dx.splits > 1 || p.few || p.piece < vocab ? (size_t)rows * p.pitch * 4 * p.dx.splits : 0);
         take(p.dw_slab, p.dw.splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw.splits : 0);
     }
-    take(p.xcopy, (size_t)p.krows * p.pitch * 2 * p.limbs);
+    if (p.few) take(p.xpack, (size_t)up(width, 32) * 16 * few_tiles(rows) * few_groups(rows) * 2 * p.limbs);
+    take(p.xcopy, p.few && (!bwd || p.few_dw) ? 0 : (size_t)p.krows * p.pitch * 2 * p.limbs);
     if (!p.few) take(p.wcopy, (size_t)up(p.piece, 32) * p.pitch * 2 * p.limbs);
     p.total = at;
     return p;
@@ -899,12 +972,17 @@ static hipError_t launch_both(XentMm dx, XentMm dw, hipStream_t st)
 
 // z of all classes into a slab
 template <typename T>
-static hipError_t launch_few_z(const uint16_t *x, int64_t xlimb, int pitch, const T *w, float *z, int rows, int width, int vocab, hipStream_t st)
+static hipError_t launch_few_z(const T *x, char *packed, const T *w, float *z, int rows, int width, int vocab, hipStream_t st)
 {
-    const dim3 grid((unsigned)((vocab + 127) / 128));
-    const int ld = (int)up(vocab, 8), mt = few_tiles(rows);
-    const auto kernel = mt == 1 ? xent_few_z<T, 1> : mt == 2 ? xent_few_z<T, 2> : xent_few_z<T, 4>;
-    NGC_LAUNCH(kernel, grid, dim3(256), 0, st, x, xlimb, pitch, w, z, ld, rows, width, vocab);
+    const int ld = (int)up(vocab, 8), mt = few_tiles(rows), classes = 16 * xent_few_blocks(mt);
+    uint4 *xp = reinterpret_cast<uint4 *>(packed);
+    NGC_LAUNCH((xent_pack<T>), dim3((unsigned)((width + 31) / 32)), dim3(256), 0, st, x, xp, rows, width, mt * few_groups(rows));
+    const hipError_t e = launch_result();
+    if (e != hipSuccess) return e;
+    auto kernel = mt == 1 ? xent_few_z<T, 1> : xent_few_z<T, 2>;
+    if constexpr (sizeof(T) == 4)
+        if (mt == 4) kernel = xent_few_z<T, 4>;
+    NGC_LAUNCH(kernel, dim3((unsigned)((vocab + classes - 1) / classes), few_groups(rows)), dim3(256), 0, st, xp, w, z, ld, rows, width, vocab);
     return launch_result();
 }
 
@@ -912,9 +990,11 @@ template <typename T>
 static hipError_t launch_few_dx(const uint16_t *g, int64_t glimb, int gp, const T *w, float *slab, int pitch, int rows, int width, int vocab, int splits,
                                 hipStream_t st)
 {
-    const dim3 grid((unsigned)((width + 63) / 64), (unsigned)splits);
+    const dim3 grid((unsigned)((width + 63) / 64), (unsigned)splits, few_groups(rows));
     const int per = (int)up(((int64_t)vocab + splits - 1) / splits, 128), mt = few_tiles(rows);
-    const auto kernel = mt == 1 ? xent_few_dx<T, 1> : mt == 2 ? xent_few_dx<T, 2> : xent_few_dx<T, 4>;
+    auto kernel = mt == 1 ? xent_few_dx<T, 1> : xent_few_dx<T, 2>;
+    if constexpr (sizeof(T) == 4)
+        if (mt == 4) kernel = xent_few_dx<T, 4>;
     NGC_LAUNCH(kernel, grid, dim3(256), 0, st, g, glimb, gp, w, slab, pitch, rows, width, vocab, per);
     return launch_result();
 }
@@ -947,8 +1027,8 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
     const XentPlan pl = xent_plan(sizeof(T) == 4 ? NGC_F32 : NGC_BF16, rows, width, vocab, false);
     const bool copy_w = pl.copy || (reinterpret_cast<uintptr_t>(w) & 15) != 0;
     XentMm p{};
-    hipError_t e = operand(pl, x, ws + pl.xcopy, rows, rows, width, p.mm.a, st);
-    if (e != hipSuccess) return e;
+    hipError_t e = hipSuccess;
+    if (!pl.few && (e = operand(pl, x, ws + pl.xcopy, rows, rows, width, p.mm.a, st)) != hipSuccess) return e;
     p.mm.lda = p.mm.ldb = pl.pitch;
     p.mm.M = rows; p.mm.K = pl.pitch; p.mm.splits = 1;
     p.mm.alimb = (int64_t)rows * pl.pitch;
@@ -958,7 +1038,7 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
     if (pl.few) {
         float *z = reinterpret_cast<float *>(ws + pl.zslab);
         const int ld = (int)up(vocab, 8);
-        if ((e = launch_few_z(p.mm.a, p.mm.alimb, pl.pitch, w, z, rows, width, vocab, st)) != hipSuccess) return e;
+        if ((e = launch_few_z(x, ws + pl.xpack, w, z, rows, width, vocab, st)) != hipSuccess) return e;
         return row_loss(z, 1, rows, ld, labels, loss, lse, vocab, st);
     }
     int tiles = 0;
@@ -1011,8 +1091,8 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
         NGC_LAUNCH(xent_rows, dim3(grid), dim3(1024), 0, st, labels, lse, dloss, tops, grid > 1 ? grid : 0, info, scale, rows, vocab);
         if ((e = launch_result()) != hipSuccess) return e;
     }
-    const uint16_t *xp, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
-    if ((e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
+    const uint16_t *xp = nullptr, *wp, *g = reinterpret_cast<const uint16_t *>(ws + pl.g);
+    if ((!pl.few || (dw && !pl.few_dw)) && (e = operand(pl, x, ws + pl.xcopy, rows, pl.krows, width, xp, st)) != hipSuccess) return e;
     const bool one = pl.dx.splits == 1 && !pl.few;                       // dx leaves the products whole
     const bool together = dx && dw && !pl.few && pl.piece >= vocab && pl.dw.splits == 1 && pl.dx.edge == pl.dw.edge && pl.dw.edge < 256;
     for (int64_t v0 = 0; v0 < vocab; v0 += pl.piece) {
@@ -1033,7 +1113,7 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             q.slab = reinterpret_cast<float *>(ws + pl.zslab);
             q.ldo = q.store_n = ld; q.store_m = rows;
             q.mm.splits = pl.z.splits;
-            e = pl.few ? launch_few_z(xp, q.mm.alimb, pl.pitch, w, q.slab, rows, width, vocab, st) : launch_mm<T, false, false, XE_SLAB>(q, pl.z.edge, st);
+            e = pl.few ? launch_few_z(x, ws + pl.xpack, w, q.slab, rows, width, vocab, st) : launch_mm<T, false, false, XE_SLAB>(q, pl.z.edge, st);
             if (e != hipSuccess) return e;
             const auto kernel = vocab > XENT_WIDE ? xent_row_grad<T, 16> : xent_row_grad<T, 4>;
             NGC_LAUNCH(kernel, dim3((unsigned)pl.krows), dim3(vocab > XENT_WIDE ? 1024 : 256), 0, st, q.slab, pl.z.splits, (size_t)rows * ld, ld, labels, lse, dloss,
@@ -1062,9 +1142,11 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             if (e != hipSuccess) return e;
             both = q;
         }
-        if (dw && pl.few && rows <= 16) {
+        if (dw && pl.few_dw) {
             const int lanes = width <= 64 ? 16 : width <= 256 ? 64 : 256;
-            const auto kernel = lanes == 16 ? xent_few_dw<T, 16> : lanes == 64 ? xent_few_dw<T, 64> : xent_few_dw<T, 256>;
+            auto kernel = lanes == 16 ? xent_few_dw<T, 16, 16> : lanes == 64 ? xent_few_dw<T, 16, 64> : xent_few_dw<T, 16, 256>;
+            if constexpr (sizeof(T) == 4)
+                if (rows > 16) kernel = lanes == 16 ? xent_few_dw<T, 32, 16> : lanes == 64 ? xent_few_dw<T, 32, 64> : xent_few_dw<T, 32, 256>;
             NGC_LAUNCH(kernel, dim3((unsigned)((vocab + 63) / 64), (unsigned)((width + 4 * lanes - 1) / (4 * lanes))), dim3(256), 0, st, g, p.glimb, gp, x, scale, dw,
                        rows, width, vocab);
             if ((e = launch_result()) != hipSuccess) return e;

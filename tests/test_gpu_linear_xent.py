@@ -209,3 +209,12 @@ def test_weights_of_rows_that_do_not_count(rows, vocab):
         got.append((dx, dw))
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
     assert bool((got[0][0][torch.from_numpy(dead).cuda()] == 0).all())
+
+
+# two groups of rows, and the sizes around the ends of the rules
+@pytest.mark.parametrize("dtype,rows,width,vocab", [("f32", 128, 515, 8200), ("f32", 97, 64, 9001), ("f32", 129, 40, 8300), ("f32", 32, 31, 8192), ("f32", 24, 1025, 8201),
+                                                    ("bf16", 32, 131, 8195), ("bf16", 33, 131, 8195), ("f32", 100, 3, 8193), ("bf16", 9, 2, 8211)])
+def test_few_rows_in_groups(dtype, rows, width, vocab):
+    print(f"linear_xent groups {rows} {width} {vocab} {dtype}", flush=True)
+    _check(dtype, *_inputs(dtype, rows, width, vocab, 84 + rows))
+    _check(dtype, *_inputs(dtype, rows, width, vocab, 85 + rows), offset=1)
