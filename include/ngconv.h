@@ -325,7 +325,8 @@ const char *ngc_conv3d_kernel(const ngc_conv3d_desc *desc, int op);
  * The nodes at both ends of a model over a vocabulary, next to the Softmax row op: rows from tokens, normalised rows, and the loss of
  * the last linear layer; derivative nodes as in Sec. 3.  Tensors are dense and element aligned (ids and labels 8 bytes, fp32 vectors
  * 4 bytes, ws 16 bytes); every [rows, cols] tensor holds fewer than 2^40 elements and has fewer than 2^31 rows.  Sums and statistics
- * are fp32, results of `dtype` are rounded once, and a result does not depend on timing.  Inputs must be finite. */
+ * are fp32, results of `dtype` are rounded once, and a result does not depend on timing.  Inputs must be finite; outputs and ws overlap
+ * no input unless it says so. */
 
 /* Embedding lookup: y[t] = scale * table[ids[t]], table: [vocab, width], y: [tokens, width], both of `dtype`.  A token whose id is
  * outside [0, vocab) has no row (padding): y[t] = +0. */
@@ -365,7 +366,7 @@ int ngc_linear_xent(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, c
 
 /* Its gradients: g[n][v] = (exp(z[n][v] - lse[n]) - [v = labels[n]]) * dloss[n], 0 for the rows that do not count; dx = g w, dw = g^T x, both
  * of `dtype`, overwritten; either (not both) may be NULL.  lse: of the forward call on the same x and w; dloss: fp32 [rows] (1 / count for a
- * mean).  The logits are formed again, a piece of the vocabulary at a time.
+ * mean); neither is used in rows that do not count.  For bf16 operands g is rounded to bf16 once (2^-9 of its value).  The logits are formed again, a piece of the vocabulary at a time.
  * ws: ngc_linear_xent_workspace_bytes(dtype, rows, width, vocab, 1) bytes. */
 int ngc_linear_xent_bwd(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, const void *x, const void *w, const int64_t *labels,
                         const float *lse, const float *dloss, void *dx, void *dw, void *ws, size_t ws_bytes, void *hip_stream);

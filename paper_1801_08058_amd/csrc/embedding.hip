@@ -6,8 +6,10 @@
 
 namespace ngc {
 
-// Bound: HBM.  GL lanes per token, 16 bytes a lane and step; rows of no multiple of 16 bytes end in a vector that overlaps the one before it
-// (both hold the same values), rows below 16 bytes go element by element.
+// Bound: HBM (32768 rows of 4096 bf16 out of 50257: 59 us, 4.5 TB/s written; 143 MB of the 268 read come from it, frequent rows from the caches).
+// GL lanes per token, as many as a row has vectors, so that every lane has work and a long row's loads are under way together; 16 bytes a lane and
+// step.  Rows of no multiple of 16 bytes end in a vector that overlaps the one before it (both hold the same values), rows below 16 bytes go element
+// by element.
 template <typename T, int GL>
 __global__ __launch_bounds__(256) void embedding_rows(const T *__restrict__ table, const int64_t *__restrict__ ids, T *__restrict__ y, int64_t tokens,
                                                       int vocab, int width, float scale, int whole)
@@ -75,7 +77,8 @@ hipError_t launch_embedding(int dtype, int64_t tokens, int vocab, int width, flo
 // Up to 8192 tokens take three launches: each range looks through all tokens itself (from the L2), which costs less than a launch that sorts
 // blocks (5001 tokens, 10007 rows of 777, fp32, all launches: 31.8 -> 27 us; 18935 tokens: 7.6 us for launch 1 alone).  Above,
 // the looking grows with tokens x ranges.
-// Bound: HBM, dy read once and dtable written once.
+// Bound: HBM, dy read once and dtable written once (16384 tokens of 2048 bf16 over 32000 rows: 91 us for 329 MB; launches 11, 50 with the zeros of
+// 25000 rows, 6 and 28 us).
 constexpr int EMB_RANGES = 2048, EMB_BLOCKS = 512, EMB_TILE = 2048, EMB_SCAN = 8192;
 constexpr int EMB_MOST = 1 << 10;                        // ids of a range at most
 

@@ -6,6 +6,10 @@
 // The logits are never kept: the forward pass leaves of every tile the maximum and the sum of each row; the backward pass forms g again
 // for a piece of the vocabulary at a time.  All products run on the bf16 matrix cores (mm_bf16.h); fp32 tensors as three limbs of bf16, which
 // six products of limbs multiply as exactly as fp32 arithmetic does, at a sixth of the bf16 rate: the fp32 matrix instructions have a sixteenth.
+//
+// Bound: matrix pipes; few rows HBM, the weight read once per product (1 x 4096 over 50257 classes bf16: 90 us, 4.5 TB/s); few rows and classes
+// the chain of launches (128 x 2048 over 1000 classes: five of 4 to 9 us).  8192 x 4096 over 50257 classes bf16: loss 2.7 ms, with gradients 10.5 ms
+// of which the logits, formed again, are 2.8.
 #include "mm_bf16.h"
 #include "rows.h"
 
@@ -818,7 +822,7 @@ struct MmChoice {
 };
 
 // From the tiles of the fullest compute unit: a start and an end per tile and a time per stage of 32.  Two workgroups of a 128 tile and four of a
-// 64 tile share a compute unit and hide each other's waits (three limbs: one and two).
+// 64 tile share a compute unit and hide each other's waits (three limbs: one and two).  Fitted to times with each tile forced.
 static float mm_expected(int edge, int limbs, int64_t m, int64_t n, int64_t stages, int splits)
 {
     const int64_t tiles = ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * splits, per_cu = (tiles + 255) / 256;

@@ -22,6 +22,7 @@ namespace ngc {
 // A long bf16 row stays packed between the passes over it: unpacked (and its exponentials taken) again instead of kept as
 // floats, so that twice as many rows are in flight on a compute unit (1047 x 32029: 36.2 -> 30.3 us).  fp32 exponentials
 // replace the elements; of a short bf16 row they are kept (32768 x 1000: 20.1 us against 21.6 us).
+//
 // The row in registers: V vectors per lane of a group of GL lanes: E <= cols <= GL * E * V.  TAIL: cols is no multiple of E
 // or the tensors are off the 16-byte grid.  BWD: a = y, b = dy, out = dx; else a = x, out = y (b unused).
 template <typename T, int V, bool BWD, int GL, bool TAIL>
