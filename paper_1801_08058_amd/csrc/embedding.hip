@@ -307,7 +307,7 @@ __device__ __forceinline__ void sort_range(unsigned lo, unsigned hi, F entry, un
     // against all lanes on a row).  Rows of whole 128-byte lines are streamed past the cache, which keeps dy there (16384 tokens bf16, 32000 rows
     // of 2048, all launches: 98 -> 91 us); lines that two rows share are not (206 MB of rows of 2209: 60 us streamed, 32 us through the cache)
     const bool lines = (width & 31) == 0 && (reinterpret_cast<uintptr_t>(dtable) & 127) == 0;
-    const int lanes = width <= 32 ? 8 : width <= 256 ? 64 : 256;
+    const int lanes = width <= 32 ? 8 : width <= 1024 ? 64 : 256;
     const uint64_t skew = (reinterpret_cast<uintptr_t>(dtable) >> 2) & 3;
     float *const grid16 = dtable - skew;
     for (int r = threadIdx.x / lanes; r < size; r += 256 / lanes) {
@@ -364,14 +364,19 @@ __global__ __launch_bounds__(256) void embedding_sort_ranges(const uint2 *__rest
     sort_range(lo, hi, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
 }
 
+static unsigned scan_lds(int tokens, int shift) { return ((tokens + 255) / 256 * 256 + (4 << shift) + 4) * 4 + (1 << shift); }
+
 // SCAN: a wave looks through a quarter of the tokens, keeps those of the range in their order and counts those of lower ids
 __global__ __launch_bounds__(256) void embedding_sort_scan(const int64_t *__restrict__ ids, unsigned *__restrict__ byid, unsigned *__restrict__ rowstart,
                                                            float *__restrict__ dtable, int tokens, int vocab, int width, int shift)
 {
-    __shared__ unsigned list[4][EMB_SCAN / 4], cnt[4 * EMB_MOST], sm[4];
-    __shared__ uint8_t none[EMB_MOST];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, range = blockIdx.x;
-    const int share = (tokens + 255) / 256 * 64, t0 = wave * share, t1 = t0 + share < tokens ? t0 + share : tokens;
+    // as much LDS as the sizes need: few tokens leave room for eight workgroups on a compute unit
+    extern __shared__ unsigned space[];                  // scan_lds words
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, range = blockIdx.x, size = 1 << shift;
+    const int share = (tokens + 255) / 256 * 64;
+    unsigned *const list = space + wave * share, *const cnt = space + 4 * share, *const sm = cnt + 4 * size;
+    uint8_t *const none = reinterpret_cast<uint8_t *>(sm + 4);
+    const int t0 = wave * share, t1 = t0 + share < tokens ? t0 + share : tokens;
     unsigned mine = 0, lower = 0;
     for (int t = t0; t < t1; t += 512) {
         int64_t id[8];
@@ -382,7 +387,7 @@ __global__ __launch_bounds__(256) void embedding_sort_scan(const int64_t *__rest
             const bool live = id[k] >= 0 && id[k] < vocab;
             const int r = live ? (int)(id[k] >> shift) : -1;
             const uint64_t here = __ballot(r == range);
-            if (r == range) list[wave][mine + __popcll(here & ((1ull << lane) - 1))] = (unsigned)(t + 64 * k + lane) << 16 | ((unsigned)id[k] & ((1u << shift) - 1));
+            if (r == range) list[mine + __popcll(here & ((1ull << lane) - 1))] = (unsigned)(t + 64 * k + lane) << 16 | ((unsigned)id[k] & ((1u << shift) - 1));
             mine += __popcll(here);
             lower += __popcll(__ballot(live && r < range));
         }
@@ -390,7 +395,7 @@ __global__ __launch_bounds__(256) void embedding_sort_scan(const int64_t *__rest
     unsigned base, all;
     (void)block_scan<4>(lane == 0 ? lower : 0, sm, base);
     (void)block_scan<4>(lane == 0 ? mine : 0, sm, all);
-    auto entry = [&](unsigned e) { return make_uint2(list[wave][e] >> 16, list[wave][e] & 0xFFFFu); };
+    auto entry = [&](unsigned e) { return make_uint2(list[e] >> 16, list[e] & 0xFFFFu); };
     sort_range(0, mine, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
 }
 
@@ -492,7 +497,7 @@ static hipError_t launch_embedding_bwd_t(int64_t tokens, int vocab, int width, f
     float *sums = reinterpret_cast<float *>(ws + p.sums);
     hipError_t e;
     if (p.scan) {
-        NGC_LAUNCH(embedding_sort_scan, dim3(p.ranges), dim3(256), 0, st, ids, byid, rowstart, dtable, (int)tokens, vocab, width, p.shift);
+        NGC_LAUNCH(embedding_sort_scan, dim3(p.ranges), dim3(256), scan_lds((int)tokens, p.shift), st, ids, byid, rowstart, dtable, (int)tokens, vocab, width, p.shift);
     } else {
         int bits = 0;
         while ((1 << bits) < p.ranges) ++bits;
