@@ -77,9 +77,12 @@ hipError_t launch_embedding(int dtype, int64_t tokens, int vocab, int width, flo
 // Up to 8192 tokens take three launches: each range looks through all tokens itself (from the L2), which costs less than a launch that sorts
 // blocks (5001 tokens, 10007 rows of 777, fp32, all launches: 31.8 -> 27 us; 18935 tokens: 7.6 us for launch 1 alone).  Above,
 // the looking grows with tokens x ranges.
-// Bound: HBM, dy read once and dtable written once (16384 tokens of 2048 bf16 over 32000 rows: 91 us for 329 MB; launches 11, 50 with the zeros of
-// 25000 rows, 6 and 28 us).
+// Bound: HBM, dy read once and dtable written once (16384 tokens of 2048 bf16 over 32000 rows: 88 us for 329 MB; launches 10, 44 with the zeros of
+// 25000 rows, 6 and 27 us).
 constexpr int EMB_RANGES = 2048, EMB_BLOCKS = 512, EMB_TILE = 2048, EMB_SCAN = 8192;
+// Waves of a range's workgroup: the range of the frequent ids may hold a third of the tokens (18935 tokens, 18913 rows of 64: launch 2 takes 26 us
+// with four, 17 with eight)
+constexpr int EMB_WAVES = 8;
 constexpr int EMB_MOST = 1 << 10;                        // ids of a range at most
 
 struct EmbPlan {
@@ -247,14 +250,14 @@ __global__ __launch_bounds__(512) void embedding_sort_blocks(const int64_t *__re
     }
 }
 
-// Second half of the sort, by a workgroup of 256: the tokens of a range, of which wave w holds entries lo .. hi - 1 (token, id within the range), all
-// waves' in the tokens' order; base: tokens of lower ids.  cnt: 4 x size words, none: size bytes, sm: 4 words of LDS.
-template <class F>
+// Second half of the sort, by a workgroup of NW waves: the tokens of a range, of which wave w holds entries lo .. hi - 1 (token, id within the range), all
+// waves' in the tokens' order; base: tokens of lower ids.  cnt: NW x size words, none: size bytes, sm: NW words of LDS.
+template <int NW, class F>
 __device__ __forceinline__ void sort_range(unsigned lo, unsigned hi, F entry, unsigned base, unsigned all, int range, bool last, int shift, unsigned *cnt, uint8_t *none,
                                            unsigned *sm, unsigned *__restrict__ byid, unsigned *__restrict__ rowstart, float *__restrict__ dtable, int vocab, int width)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, size = 1 << shift;
-    for (int i = threadIdx.x; i < 4 * size; i += 256) cnt[i] = 0;
+    for (int i = threadIdx.x; i < NW * size; i += 64 * NW) cnt[i] = 0;
     __syncthreads();
     if (size > 1) {
         for (unsigned e = lo + lane; e < hi; e += 256) {
@@ -270,20 +273,20 @@ __device__ __forceinline__ void sort_range(unsigned lo, unsigned hi, F entry, un
     }
     __syncthreads();
     unsigned sum = 0, total;
-    const int rows = (size + 255) / 256;                 // ids of a thread
+    const int rows = (size + 64 * NW - 1) / (64 * NW);                 // ids of a thread
     for (int k = 0; k < rows; ++k) {
         const int r = threadIdx.x * rows + k;
         if (r < size)
-            for (int w = 0; w < 4; ++w) sum += cnt[w * size + r];
+            for (int w = 0; w < NW; ++w) sum += cnt[w * size + r];
     }
-    unsigned at = block_scan<4>(sum, sm, total);
+    unsigned at = block_scan<NW>(sum, sm, total);
     for (int k = 0; k < rows; ++k) {
         const int r = threadIdx.x * rows + k;
         if (r >= size) break;
         const int64_t v = ((int64_t)range << shift) + r;
         if (v <= vocab) rowstart[v] = base + at;         // v = vocab: the end of the last row, if it falls inside the last range
         const unsigned begin = at;
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const unsigned c = cnt[w * size + r];
             cnt[w * size + r] = at;
             at += c;
@@ -310,7 +313,7 @@ __device__ __forceinline__ void sort_range(unsigned lo, unsigned hi, F entry, un
     const int lanes = width <= 32 ? 8 : width <= 1024 ? 64 : 256;
     const uint64_t skew = (reinterpret_cast<uintptr_t>(dtable) >> 2) & 3;
     float *const grid16 = dtable - skew;
-    for (int r = threadIdx.x / lanes; r < size; r += 256 / lanes) {
+    for (int r = threadIdx.x / lanes; r < size; r += 64 * NW / lanes) {
         if (!none[r]) continue;
         const uint64_t from = (uint64_t)(((int64_t)range << shift) + r) * width + skew, to = from + width, q0 = (from + 3) >> 2, q1 = to >> 2;
         const int l = threadIdx.x & (lanes - 1);
@@ -322,36 +325,27 @@ __device__ __forceinline__ void sort_range(unsigned lo, unsigned hi, F entry, un
     }
 }
 
-__global__ __launch_bounds__(256) void embedding_sort_ranges(const uint2 *__restrict__ byrange, const unsigned *__restrict__ starts, unsigned *__restrict__ byid,
+__global__ __launch_bounds__(64 * EMB_WAVES) void embedding_sort_ranges(const uint2 *__restrict__ byrange, const unsigned *__restrict__ starts, unsigned *__restrict__ byid,
                                                              unsigned *__restrict__ rowstart, float *__restrict__ dtable, int vocab, int width, int shift, int blocks,
                                                              int64_t per_block)
 {
-    __shared__ unsigned pre[EMB_BLOCKS + 1], from[EMB_BLOCKS], cnt[4 * EMB_MOST], sm[4];
+    __shared__ unsigned pre[EMB_BLOCKS + 1], from[EMB_BLOCKS], cnt[EMB_WAVES * EMB_MOST], sm[EMB_WAVES];
     __shared__ uint8_t none[EMB_MOST];
     const int wave = threadIdx.x >> 6, range = blockIdx.x;
     unsigned base = 0, all = 0;
-    // segments of this range: two blocks a thread
-    unsigned s0[2], len[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int b = threadIdx.x * 2 + k;
-        s0[k] = len[k] = 0;
-        if (b < blocks) {
-            s0[k] = starts[(size_t)range * blocks + b];
-            len[k] = starts[(size_t)(range + 1) * blocks + b] - s0[k];
-        }
+    static_assert(EMB_BLOCKS == 64 * EMB_WAVES, "a block a thread");
+    // segments of this range: a block a thread
+    const int b = threadIdx.x;
+    unsigned s0 = 0, len = 0;
+    if (b < blocks) {
+        s0 = starts[(size_t)range * blocks + b];
+        len = starts[(size_t)(range + 1) * blocks + b] - s0;
     }
-    unsigned at = block_scan<4>(len[0] + len[1], sm, all);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int b = threadIdx.x * 2 + k;
-        pre[b] = at;
-        from[b] = s0[k];
-        at += len[k];
-    }
-    if (threadIdx.x == 255) pre[EMB_BLOCKS] = all;
-    (void)block_scan<4>(s0[0] + s0[1], sm, base);        // base: tokens of lower ids
-    const unsigned per_wave = (all + 255) / 256 * 64, lo = wave * per_wave, hi = lo + per_wave < all ? lo + per_wave : all;
+    pre[b] = block_scan<EMB_WAVES>(len, sm, all);
+    from[b] = s0;
+    if (b == 0) pre[EMB_BLOCKS] = all;
+    (void)block_scan<EMB_WAVES>(s0, sm, base);           // base: tokens of lower ids
+    const unsigned per_wave = (all + 64 * EMB_WAVES - 1) / (64 * EMB_WAVES) * 64, lo = wave * per_wave, hi = lo + per_wave < all ? lo + per_wave : all;
     auto entry = [&](unsigned e) {                       // the block whose segment holds entry e
         int a = 0, b = blocks;
         while (b - a > 1) {
@@ -361,7 +355,7 @@ __global__ __launch_bounds__(256) void embedding_sort_ranges(const uint2 *__rest
         }
         return byrange[a * per_block + from[a] + (e - pre[a])];
     };
-    sort_range(lo, hi, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
+    sort_range<EMB_WAVES>(lo, hi, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
 }
 
 static unsigned scan_lds(int tokens, int shift) { return ((tokens + 255) / 256 * 256 + (4 << shift) + 4) * 4 + (1 << shift); }
@@ -396,7 +390,7 @@ __global__ __launch_bounds__(256) void embedding_sort_scan(const int64_t *__rest
     (void)block_scan<4>(lane == 0 ? lower : 0, sm, base);
     (void)block_scan<4>(lane == 0 ? mine : 0, sm, all);
     auto entry = [&](unsigned e) { return make_uint2(list[e] >> 16, list[e] & 0xFFFFu); };
-    sort_range(0, mine, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
+    sort_range<4>(0, mine, entry, base, all, range, range == (int)gridDim.x - 1, shift, cnt, none, sm, byid, rowstart, dtable, vocab, width);
 }
 
 // sum[u] += rows row(lo) .. row(hi - 1) of dy, columns col[u] ..; U groups per lane.  lo and hi are the same in all lanes.  The loads of B rows are
@@ -505,7 +499,7 @@ static hipError_t launch_embedding_bwd_t(int64_t tokens, int vocab, int width, f
         if ((e = lds.raise(reinterpret_cast<const void *>(&embedding_sort_blocks))) != hipSuccess) return e;
         NGC_LAUNCH(embedding_sort_blocks, dim3(p.blocks), dim3(512), (p.ranges + 1) * 8 * 4, st, ids, byrange, starts, tokens, vocab, p.shift, bits, p.ranges, p.per_block);
         if ((e = launch_result()) != hipSuccess) return e;
-        NGC_LAUNCH(embedding_sort_ranges, dim3(p.ranges), dim3(256), 0, st, byrange, starts, byid, rowstart, dtable, vocab, width, p.shift, p.blocks, p.per_block);
+        NGC_LAUNCH(embedding_sort_ranges, dim3(p.ranges), dim3(64 * EMB_WAVES), 0, st, byrange, starts, byid, rowstart, dtable, vocab, width, p.shift, p.blocks, p.per_block);
     }
     if ((e = launch_result()) != hipSuccess) return e;
     const int groups = width < 4 ? width : width / 4 + (width % 4 != 0);
