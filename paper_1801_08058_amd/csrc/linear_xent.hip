@@ -110,11 +110,13 @@ __device__ __forceinline__ void split_limbs(const float (&f)[8], mm_bf16x8 (&out
         __builtin_memcpy(&out[q], w, 16);
     }
 }
-// c + a b^T, of three limbs the six products that mm_bf16.h forms
-template <int L>
-__device__ __forceinline__ mm_f32x4 limb_products(const mm_bf16x8 (&a)[L], const mm_bf16x8 (&b)[L], mm_f32x4 c)
+// c + a b^T: of three limbs the six products that mm_bf16.h forms, of one and two both
+template <int PA, int PB>
+__device__ __forceinline__ mm_f32x4 limb_products(const mm_bf16x8 (&a)[PA], const mm_bf16x8 (&b)[PB], mm_f32x4 c)
 {
-    if constexpr (L == 3) {
+    static_assert((PA == 1 && PB <= 2) || (PA == 3 && PB == 3), "limbs");
+    if constexpr (PB == 2) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[1], c, 0, 0, 0);
+    if constexpr (PA == 3) {
         c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[2], c, 0, 0, 0);
         c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[2], b[0], c, 0, 0, 0);
         c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1], b[1], c, 0, 0, 0);
@@ -123,6 +125,15 @@ __device__ __forceinline__ mm_f32x4 limb_products(const mm_bf16x8 (&a)[L], const
     }
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[0], c, 0, 0, 0);
 }
+
+// g as an operand of dx and dw has the three limbs of fp32 tensors, and of bf16 tensors two (16 bits) up to this many rows, one (rounded to bf16) of
+// more.  The rounding of the g at a label is the same in all elements of the row's dx that come from it, and in those of the label's dw: with one
+// limb the distance from exact gradients is 0.0018 to 0.0022 of their norm, with two the 0.0017 that rounding the results leaves (1 to 2048 rows).  Two limbs are
+// twice the matrix instructions.  Up to about this many rows memory and the launches bound dx and dw; above them those instructions do.  Loss and
+// gradients with one limb and with two, 2048 wide over 32000 classes: 111 -> 117 us for 8 rows, 152 -> 175 for 128, 207 -> 254 for 256, 0.95 -> 1.47
+// ms for 2048; 8192 x 4096 over 50257: 10.7 -> 18.3 ms.
+constexpr int XENT_FINE_ROWS = 128;
+static int xent_glimbs(int limbs, int64_t rows) { return limbs == 3 ? 3 : rows <= XENT_FINE_ROWS ? 2 : 1; }
 
 // T: uint16_t (bf16) or float (in limbs)
 enum XentEpilogue { XE_STATS, XE_GRAD, XE_SLAB, XE_OUT };
@@ -135,14 +146,18 @@ struct XentMm {
     float *target;                       // STATS
     const XentRow *info;                 // GRAD
     const float *scale;                  // OUT
-    void *out;                           // GRAD: g (bf16; fp32: its limbs, glimb elements apart), OUT: the result
+    void *out;                           // GRAD: g (its limbs, glimb elements apart), OUT: the result
     int64_t ldo, glimb;
     int store_m, store_n;                // rows and columns that are stored (GRAD: zeros past the rows and the piece)
     float *slab;                         // SLAB: [splits][M][ldo]
     int add;                             // SLAB: onto what is there; OUT: the slab ([M][N]) joins the result
 };
 
-template <typename T, int BM, int BN, bool AT, bool BT, XentEpilogue E>
+// limbs of the operands: dx and dw (BT) take g, of G limbs, first
+template <typename T, int G, bool BT> constexpr int xent_pa() { return BT ? G : sizeof(T) == 4 ? 3 : 1; }
+template <typename T> constexpr int xent_pb() { return sizeof(T) == 4 ? 3 : 1; }
+
+template <typename T, int G, int BM, int BN, bool AT, bool BT, XentEpilogue E>
 __device__ __forceinline__ void xent_product(const XentMm &p, int block)
 {
     constexpr int FM = BM / 32, FN = BN / 32;
@@ -153,7 +168,7 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
     mm_tile_of(block - split * tiles, tiles, p.mm.mt, p.mm.nt, tm, tn);
     const int k0 = split * p.mm.kper, k1 = p.mm.K - k0 < p.mm.kper ? p.mm.K : k0 + p.mm.kper;
     mm_f32x4 acc[FN][FM];
-    mm_tile<BM, BN, AT, BT, LIMBS ? 3 : 1>(p.mm, smem, tm * BM, tn * BN, k0, k1, acc);
+    mm_tile<BM, BN, AT, BT, xent_pa<T, G, BT>(), xent_pb<T>()>(p.mm, smem, tm * BM, tn * BN, k0, k1, acc);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     const int wm = (wave % 2) * (BM / 2), wn = (wave / 2) * (BN / 2);
@@ -279,14 +294,14 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
 #pragma unroll
         for (int i = 0; i < FN; i += 2)
 #pragma unroll
-            for (int l = 0; l < (E == XE_GRAD && LIMBS ? 3 : 1); ++l) {
+            for (int l = 0; l < (E == XE_GRAD ? G : 1); ++l) {
                 uint32_t q[2][2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     mm_f32x4 &v = acc[i + k][j];
                     q[k][0] = pack_bf16x2_hw(v[0], v[1]);
                     q[k][1] = pack_bf16x2_hw(v[2], v[3]);
-                    if (E == XE_GRAD && LIMBS)
+                    if (E == XE_GRAD && G > 1)
                         v -= mm_f32x4{__uint_as_float(q[k][0] << 16), __uint_as_float(q[k][0] & 0xFFFF0000u), __uint_as_float(q[k][1] << 16), __uint_as_float(q[k][1] & 0xFFFF0000u)};
                 }
                 uint32_t o[4];
@@ -311,18 +326,18 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
     }
 }
 
-template <typename T, int EDGE, bool AT, bool BT, XentEpilogue E>
+template <typename T, int G, int EDGE, bool AT, bool BT, XentEpilogue E>
 __global__ __launch_bounds__(64 * MM_WAVES) void xent_mm(const XentMm p)
 {
-    xent_product<T, EDGE, EDGE, AT, BT, E>(p, blockIdx.x);
+    xent_product<T, G, EDGE, EDGE, AT, BT, E>(p, blockIdx.x);
 }
 
 // dx and dw of one piece, which both read g: the workgroups of dx, then those of dw
-template <typename T, int EDGE, XentEpilogue EDX>
+template <typename T, int G, int EDGE, XentEpilogue EDX>
 __global__ __launch_bounds__(64 * MM_WAVES) void xent_mm_both(const XentMm dx, const XentMm dw, int first)
 {
-    if ((int)blockIdx.x < first) xent_product<T, EDGE, EDGE, false, true, EDX>(dx, blockIdx.x);
-    else xent_product<T, EDGE, EDGE, true, true, XE_OUT>(dw, blockIdx.x - first);
+    if ((int)blockIdx.x < first) xent_product<T, G, EDGE, EDGE, false, true, EDX>(dx, blockIdx.x);
+    else xent_product<T, G, EDGE, EDGE, true, true, XE_OUT>(dw, blockIdx.x - first);
 }
 
 // Few tiles: the logits' product runs in parts (fp32 slabs, `stride` elements apart, rows of `ld`), and a workgroup per row adds them up.
@@ -389,7 +404,7 @@ __global__ __launch_bounds__(64 * NW) void xent_row_loss(const float *__restrict
 }
 
 // g of a row, as xent_rows and the epilogue of the product form it; rows from `rows` on are zeros.  Workgroup 0 leaves the scale.
-template <typename T, int NW>
+template <int G, int NW>
 __global__ __launch_bounds__(64 * NW) void xent_row_grad(const float *__restrict__ slab, int splits, size_t stride, int ld, const int64_t *__restrict__ labels,
                                                          const float *__restrict__ lse, const float *__restrict__ dloss, uint16_t *__restrict__ g,
                                                          int64_t glimb, int gp, float *__restrict__ scale, int rows, int vocab)
@@ -426,7 +441,7 @@ __global__ __launch_bounds__(64 * NW) void xent_row_grad(const float *__restrict
             for (int e = 0; e < 4; ++e)
                 z[b][e] = live && v + e < vocab ? __builtin_amdgcn_exp2f(fmaf(z[b][e], LOG2E, -lse2)) * factor - (label == v + e ? factor : 0.f) : 0.f;
 #pragma unroll
-            for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
+            for (int l = 0; l < G; ++l) {
                 const uint2 q = make_uint2(pack_bf16x2_hw(z[b][0], z[b][1]), pack_bf16x2_hw(z[b][2], z[b][3]));
                 *reinterpret_cast<uint2 *>(g + l * glimb + (size_t)m * gp + v) = q;
                 z[b] -= mm_f32x4{__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xFFFF0000u), __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xFFFF0000u)};
@@ -475,6 +490,8 @@ struct Eight {
         }
     }
 };
+
+template <typename T> constexpr int few_g() { return sizeof(T) == 4 ? 3 : 2; }          // limbs of g: bf16 has fewer than XENT_FINE_ROWS rows here
 
 // blocks of 16 classes of a workgroup: more rows of x, which every workgroup reads, more classes for them
 constexpr int xent_few_blocks(int mt) { return mt == 1 ? 2 : 4; }
@@ -580,7 +597,7 @@ template <typename T, int MT>
 __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ gr, int64_t glimb, int gp, const T *__restrict__ w, float *__restrict__ slab,
                                                    int pitch, int rows, int width, int vocab, int per_part)
 {
-    constexpr int L = sizeof(T) == 4 ? 3 : 1;
+    constexpr int L = sizeof(T) == 4 ? 3 : 1, G = few_g<T>();
     __shared__ mm_f32x4 sums[3][4 * MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
     const int d = blockIdx.x * 64 + 4 * l, m0 = blockIdx.z * 16 * MT, end = per_part * (blockIdx.y + 1) < vocab ? per_part * (blockIdx.y + 1) : vocab;
@@ -597,7 +614,7 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
     // 131 us for 54005 classes of 2541); bf16 steps are half as long, three ahead and g with them (146 -> 80 us).
     struct Step {
         uint32_t w[8][sizeof(T)];                                                // four elements
-        uint4 g[L == 1 ? MT : 1];
+        uint4 g[L == 1 ? MT : 1][G];
     };
     const int from = d + 4 <= width ? d : width - 4, shift = d - from;
     auto load = [&](Step &to, int v0) {
@@ -614,7 +631,9 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
         }
         if constexpr (L == 1)
 #pragma unroll
-            for (int j = 0; j < MT; ++j) to.g[j] = *reinterpret_cast<const uint4 *>(xr[j] + v0 + 8 * g);
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int q = 0; q < G; ++q) to.g[j][q] = *reinterpret_cast<const uint4 *>(xr[j] + q * glimb + v0 + 8 * g);
     };
     const bool edge = width < 4 ? l != 0 : shift != 0, edges = __any(edge);
     auto products = [&](const Step &now, int v0) {
@@ -632,12 +651,12 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
                 e[k] = width < 4 || shift > 3 ? make_float4(0.f, 0.f, 0.f, 0.f)
                                               : make_float4(shift == 1 ? q.y : shift == 2 ? q.z : q.w, shift == 1 ? q.z : shift == 2 ? q.w : 0.f, shift == 1 ? q.w : 0.f, 0.f);
             }
-        mm_bf16x8 b[MT][L];
+        mm_bf16x8 b[MT][G];
 #pragma unroll
         for (int j = 0; j < MT; ++j)
 #pragma unroll
-            for (int q = 0; q < L; ++q)
-                if constexpr (L == 1) b[j][q] = __builtin_bit_cast(mm_bf16x8, now.g[j]);
+            for (int q = 0; q < G; ++q)
+                if constexpr (L == 1) b[j][q] = __builtin_bit_cast(mm_bf16x8, now.g[j][q]);
                 else b[j][q] = *reinterpret_cast<const mm_bf16x8 *>(xr[j] + q * glimb + v0 + 8 * g);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -709,7 +728,7 @@ __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ 
         float s = 0.f;
         if (m < rows)
 #pragma unroll
-            for (int q = (sizeof(T) == 4 ? 3 : 1) - 1; q >= 0; --q) s += bf16_bits_to_float(gr[q * glimb + (size_t)m * gp + v0 + v]);        // gp is a multiple of 64
+            for (int q = few_g<T>() - 1; q >= 0; --q) s += bf16_bits_to_float(gr[q * glimb + (size_t)m * gp + v0 + v]);        // gp is a multiple of 64
         gs[v][m] = s * sc;
     }
     float4 f[R];
@@ -822,31 +841,32 @@ struct MmChoice {
 };
 
 // From the tiles of the fullest compute unit: a start and an end per tile and a time per stage of 32.  Two workgroups of a 128 tile and four of a
-// 64 tile share a compute unit and hide each other's waits (three limbs: one and two).  Fitted to times with each tile forced.
+// 64 tile share a compute unit and hide each other's waits (three limbs: one and two).  Fitted to times with each tile forced.  limbs: of the first operand.
 static float mm_expected(int edge, int limbs, int64_t m, int64_t n, int64_t stages, int splits)
 {
     const int64_t tiles = ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * splits, per_cu = (tiles + 255) / 256;
     const float s = (float)((stages + splits - 1) / splits), t = (float)per_cu;
     if (limbs == 3) return edge == 128 ? t * (5.f + 1.1f * s) : per_cu == 1 ? 3.f + 0.5f * s : t * (1.f + 0.38f * s);
+    if (limbs == 2) return edge == 128 ? (float)(per_cu / 2) * (3.f + 1.1f * s) + (float)(per_cu % 2) * (2.5f + 0.78f * s) : per_cu == 1 ? 2.f + 0.25f * s : t * (0.6f + 0.18f * s);
     if (edge == 256) return t * (10.f + 0.85f * s);
     if (edge == 128) return (float)(per_cu / 2) * (3.f + 0.54f * s) + (float)(per_cu % 2) * (2.5f + 0.39f * s);
     return per_cu == 1 ? 2.f + 0.2f * s : t * (0.6f + 0.115f * s);
 }
 
-// most: parts at most; slab: also a single part is written and read again as fp32
-static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int limbs, int most, bool slab)
+// pa, pb: limbs of the operands; most: parts at most; slab: also a single part is written and read again as fp32
+static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int pa, int pb, int most, bool slab)
 {
     static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     const int64_t stages = (k + 31) / 32;
     // what memory takes for the operands: a small tile is no faster than a large one then
-    const float bytes = ((float)m + (float)n) * (float)k * 2.f * (float)limbs / 4.4e6f;
+    const float bytes = ((float)m * (float)pa + (float)n * (float)pb) * (float)k * 2.f / 4.4e6f;
     MmChoice best = {64, 1, INFINITY};
     const char *forced = env_switch(SW_XENT_TILE);
-    for (int edge = limbs == 3 || slab ? 128 : 256; edge >= 64; edge /= 2)
+    for (int edge = pa > 1 || slab ? 128 : 256; edge >= 64; edge /= 2)
         for (int p : parts) {
             if (p > most || (p > 1 && k / p < 128)) break;
             if (edge < 128 && ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * p > (1 << 22)) break;      // a grid holds fewer than 2^32 threads
-            const float run = mm_expected(edge, limbs, m, n, stages, p), t = (run > bytes ? run : bytes) + (p > 1 || slab ? 3.f + (float)m * (float)n * 8.f * (float)p / 4e6f : 0.f);
+            const float run = mm_expected(edge, pa, m, n, stages, p), t = (run > bytes ? run : bytes) + (p > 1 || slab ? 3.f + (float)m * (float)n * 8.f * (float)p / 4e6f : 0.f);
             if (t < best.us && (!forced || atoi(forced) == edge || (slab && best.us == INFINITY))) best = {edge, p, t};
         }
     return best;
@@ -855,7 +875,7 @@ static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int limbs, int most, 
 // How a call goes through the vocabulary.  Pieces are as large as 512 MiB of g, and of a copy of w, allow.
 struct XentPlan {
     bool copy;                   // x and w are copied first: fp32, or rows of no multiple of 16 bytes (tensors off that grid are as well)
-    int limbs, pitch, piece;     // limbs of an element; elements of a row of x and w as the products read them; classes of a piece
+    int limbs, glimbs, pitch, piece;     // limbs of an element and of g; elements of a row of x and w as the products read them; classes of a piece
     int64_t krows;               // rows as the products count them where they are the reduction
     MmChoice z, dx, dw;          // products of a whole piece
     bool by_rows;                // z in slabs, then a workgroup per row
@@ -879,26 +899,27 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
 {
     XentPlan p{};
     p.limbs = dtype == NGC_F32 ? 3 : 1;
+    p.glimbs = xent_glimbs(p.limbs, rows);
     p.pitch = (int)up(width, p.limbs == 3 ? 32 : 8);
     p.copy = p.limbs == 3 || p.pitch != width;
     p.krows = p.limbs == 3 ? up(rows, 32) : rows;
-    const int64_t most = ((int64_t)512 << 20) / 2 / p.limbs;             // elements
+    const int64_t most = ((int64_t)512 << 20) / 2;                       // bf16 values
     int64_t piece = vocab;
-    if (bwd && piece > most / p.krows) piece = most / p.krows;
-    if (piece > most / p.pitch) piece = most / p.pitch;
+    if (bwd && piece > most / p.glimbs / p.krows) piece = most / p.glimbs / p.krows;
+    if (piece > most / p.limbs / p.pitch) piece = most / p.limbs / p.pitch;
     if (piece > (1 << 21)) piece = 1 << 21;                              // offsets in a tile of g stay below 2 GiB
     p.piece = (int)(piece >= vocab ? vocab : piece < 256 ? 256 : piece / 256 * 256);
     if (p.piece > vocab) p.piece = vocab;
     // only copies and gradients make pieces of the vocabulary (copies are also made of tensors off the 16-byte grid)
-    p.z = mm_choose(rows, p.piece, p.pitch, p.limbs, 1, false);
+    p.z = mm_choose(rows, p.piece, p.pitch, p.limbs, p.limbs, 1, false);
     if (bwd) {
-        p.dx = mm_choose(rows, p.pitch, p.piece, p.limbs, 64, false);
-        p.dw = mm_choose(p.piece, p.pitch, rows, p.limbs, 64, false);
+        p.dx = mm_choose(rows, p.pitch, p.piece, p.glimbs, p.limbs, 64, false);
+        p.dw = mm_choose(p.piece, p.pitch, rows, p.glimbs, p.limbs, 64, false);
     }
     // One piece of few tiles: in parts, as long as these take no more than 32 MiB and (backprop: every row looks at all weights) the rows are few.
     // Two launches either way.
     if (p.piece == vocab && rows <= 1024) {
-        const MmChoice parts = mm_choose(rows, vocab, p.pitch, p.limbs, 64, true);
+        const MmChoice parts = mm_choose(rows, vocab, p.pitch, p.limbs, p.limbs, 64, true);
         p.by_rows = parts.us < p.z.us && (int64_t)rows * up(vocab, 8) * 4 * parts.splits <= (32 << 20);
         if (p.by_rows) p.z = parts;
     }
@@ -912,7 +933,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         p.dx = {64, 512 / blocks < 1 ? 1 : 512 / blocks, 0.f};
         if (p.dx.splits > most) p.dx.splits = most;
         if (p.dx.splits > 64) p.dx.splits = 64;
-        if (bwd) p.dw = mm_choose(vocab, p.pitch, rows, p.limbs, 1, false);
+        if (bwd) p.dw = mm_choose(vocab, p.pitch, rows, p.glimbs, p.limbs, 1, false);
     }
     size_t at = 0;
     auto take = [&](size_t &where, size_t bytes) { where = at; at += r256(bytes); };
@@ -924,7 +945,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         take(p.info, (size_t)rows * sizeof(XentRow));
         take(p.scale, 4);
         take(p.tops, rows > XENT_ROWS ? XENT_TOPS * 4 : 0);
-        take(p.g, (size_t)p.krows * up(p.piece, 64) * 2 * p.limbs);
+        take(p.g, (size_t)p.krows * up(p.piece, 64) * 2 * p.glimbs);
         take(p.dx_slab, p.dx.splits > 1 || p.few || p.piece < vocab ? (size_t)rows * p.pitch * 4 * p.dx.splits : 0);
         take(p.dw_slab, p.dw.splits > 1 ? (size_t)p.piece * p.pitch * 4 * p.dw.splits : 0);
     }
@@ -943,34 +964,35 @@ static unsigned mm_grid(MmParams &mm, int edge)
     return (unsigned)mm.mt * (unsigned)mm.nt * (unsigned)mm.splits;
 }
 
-template <typename T, int EDGE, bool AT, bool BT, XentEpilogue E>
+template <typename T, int G, int EDGE, bool AT, bool BT, XentEpilogue E>
 static hipError_t launch_mm_tile(XentMm p, hipStream_t st)
 {
     static LdsLimitOnce lds;
-    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<T, EDGE, AT, BT, E>));
+    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm<T, G, EDGE, AT, BT, E>));
     if (e != hipSuccess) return e;
     const unsigned grid = mm_grid(p.mm, EDGE);
-    NGC_LAUNCH((xent_mm<T, EDGE, AT, BT, E>), dim3(grid), dim3(64 * MM_WAVES),
-               (mm_lds_bytes<EDGE, EDGE, sizeof(T) == 4 ? 3 : 1>()), st, p);
+    NGC_LAUNCH((xent_mm<T, G, EDGE, AT, BT, E>), dim3(grid), dim3(64 * MM_WAVES),
+               (mm_lds_bytes<EDGE, EDGE, xent_pa<T, G, BT>(), xent_pb<T>()>()), st, p);
     return launch_result();
 }
 
-template <typename T, bool AT, bool BT, XentEpilogue E>
+// G: limbs of g (of the products that neither form nor read it: any)
+template <typename T, int G, bool AT, bool BT, XentEpilogue E>
 static hipError_t launch_mm(const XentMm &p, int edge, hipStream_t st)
 {
-    if constexpr (sizeof(T) == 2 && !(E == XE_SLAB && !BT))                      // slabs of z: 128 at most
-        if (edge == 256) return launch_mm_tile<T, 256, AT, BT, E>(p, st);
-    return edge == 128 ? launch_mm_tile<T, 128, AT, BT, E>(p, st) : launch_mm_tile<T, 64, AT, BT, E>(p, st);
+    if constexpr (sizeof(T) == 2 && !(E == XE_SLAB && !BT) && !(BT && G > 1))    // slabs of z and products of two limbs: 128 at most
+        if (edge == 256) return launch_mm_tile<T, G, 256, AT, BT, E>(p, st);
+    return edge == 128 ? launch_mm_tile<T, G, 128, AT, BT, E>(p, st) : launch_mm_tile<T, G, 64, AT, BT, E>(p, st);
 }
 
-template <typename T, int EDGE, XentEpilogue EDX>
+template <typename T, int G, int EDGE, XentEpilogue EDX>
 static hipError_t launch_both(XentMm dx, XentMm dw, hipStream_t st)
 {
     static LdsLimitOnce lds;
-    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm_both<T, EDGE, EDX>));
+    const hipError_t e = lds.raise(reinterpret_cast<const void *>(&xent_mm_both<T, G, EDGE, EDX>));
     if (e != hipSuccess) return e;
     const unsigned first = mm_grid(dx.mm, EDGE), grid = first + mm_grid(dw.mm, EDGE);
-    NGC_LAUNCH((xent_mm_both<T, EDGE, EDX>), dim3(grid), dim3(64 * MM_WAVES), (mm_lds_bytes<EDGE, EDGE, sizeof(T) == 4 ? 3 : 1>()), st, dx, dw, (int)first);
+    NGC_LAUNCH((xent_mm_both<T, G, EDGE, EDX>), dim3(grid), dim3(64 * MM_WAVES), (mm_lds_bytes<EDGE, EDGE, G, xent_pb<T>()>()), st, dx, dw, (int)first);
     return launch_result();
 }
 
@@ -1058,11 +1080,11 @@ static hipError_t launch_xent_t(int rows, int width, int vocab, const T *x, cons
             p.slab = reinterpret_cast<float *>(ws + pl.zslab);
             p.ldo = p.store_n = ld; p.store_m = rows;
             p.mm.splits = pl.z.splits;
-            if ((e = launch_mm<T, false, false, XE_SLAB>(p, pl.z.edge, st)) != hipSuccess) return e;
+            if ((e = launch_mm<T, 1, false, false, XE_SLAB>(p, pl.z.edge, st)) != hipSuccess) return e;
             return row_loss(p.slab, pl.z.splits, rows, ld, labels, loss, lse, vocab, st);
         }
-        const int edge = copy_w || pl.piece == vocab ? pl.z.edge : mm_choose(rows, vocab, pl.pitch, pl.limbs, 1, false).edge;
-        if ((e = launch_mm<T, false, false, XE_STATS>(p, edge, st)) != hipSuccess) return e;
+        const int edge = copy_w || pl.piece == vocab ? pl.z.edge : mm_choose(rows, vocab, pl.pitch, pl.limbs, pl.limbs, 1, false).edge;
+        if ((e = launch_mm<T, 1, false, false, XE_STATS>(p, edge, st)) != hipSuccess) return e;
         tiles += (int)(((int64_t)p.mm.N + edge - 1) / edge);
     }
     NGC_LAUNCH(xent_join, dim3(((unsigned)rows + 31) / 32), dim3(256), 0, st, part, p.target, labels, loss, lse, rows, vocab, tiles);
@@ -1077,7 +1099,7 @@ static hipError_t sum_slabs(const float *slab, const float *scale, T *out, int r
     return launch_result();
 }
 
-template <typename T>
+template <typename T, int G>
 static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, const T *w, const int64_t *labels, const float *lse, const float *dloss,
                                     T *dx, T *dw, char *ws, hipStream_t st)
 {
@@ -1117,14 +1139,14 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             q.slab = reinterpret_cast<float *>(ws + pl.zslab);
             q.ldo = q.store_n = ld; q.store_m = rows;
             q.mm.splits = pl.z.splits;
-            e = pl.few ? launch_few_z(x, ws + pl.xpack, w, q.slab, rows, width, vocab, st) : launch_mm<T, false, false, XE_SLAB>(q, pl.z.edge, st);
+            e = pl.few ? launch_few_z(x, ws + pl.xpack, w, q.slab, rows, width, vocab, st) : launch_mm<T, 1, false, false, XE_SLAB>(q, pl.z.edge, st);
             if (e != hipSuccess) return e;
-            const auto kernel = vocab > XENT_WIDE ? xent_row_grad<T, 16> : xent_row_grad<T, 4>;
+            const auto kernel = vocab > XENT_WIDE ? xent_row_grad<G, 16> : xent_row_grad<G, 4>;
             NGC_LAUNCH(kernel, dim3((unsigned)pl.krows), dim3(vocab > XENT_WIDE ? 1024 : 256), 0, st, q.slab, pl.z.splits, (size_t)rows * ld, ld, labels, lse, dloss,
                        reinterpret_cast<uint16_t *>(ws + pl.g), p.glimb, gp, scale, rows, vocab);
             e = launch_result();
         } else {
-            e = launch_mm<T, false, false, XE_GRAD>(p, pl.z.edge, st);
+            e = launch_mm<T, G, false, false, XE_GRAD>(p, pl.z.edge, st);
         }
         if (e != hipSuccess) return e;
         XentMm both{};                                                   // dx, while it waits to run together with dw
@@ -1138,10 +1160,10 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             if (pl.dx.splits == 1 && v0 + piece >= vocab) {              // the last piece leaves the result
                 q.out = dx; q.ldo = width; q.store_n = width;
                 q.slab = dx_slab; q.add = v0 > 0;
-                if (!together) e = launch_mm<T, false, true, XE_OUT>(q, pl.dx.edge, st);
+                if (!together) e = launch_mm<T, G, false, true, XE_OUT>(q, pl.dx.edge, st);
             } else {
                 q.slab = dx_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = v0 > 0;
-                if (!together) e = launch_mm<T, false, true, XE_SLAB>(q, pl.dx.edge, st);
+                if (!together) e = launch_mm<T, G, false, true, XE_SLAB>(q, pl.dx.edge, st);
             }
             if (e != hipSuccess) return e;
             both = q;
@@ -1163,12 +1185,12 @@ static hipError_t launch_xent_bwd_t(int rows, int width, int vocab, const T *x, 
             T *out = dw + (size_t)v0 * width;
             if (pl.dw.splits == 1) {
                 q.out = out; q.ldo = width; q.store_n = width;
-                if (!together) e = launch_mm<T, true, true, XE_OUT>(q, pl.dw.edge, st);
-                else if (pl.dw.edge == 128) e = one ? launch_both<T, 128, XE_OUT>(both, q, st) : launch_both<T, 128, XE_SLAB>(both, q, st);
-                else e = one ? launch_both<T, 64, XE_OUT>(both, q, st) : launch_both<T, 64, XE_SLAB>(both, q, st);
+                if (!together) e = launch_mm<T, G, true, true, XE_OUT>(q, pl.dw.edge, st);
+                else if (pl.dw.edge == 128) e = one ? launch_both<T, G, 128, XE_OUT>(both, q, st) : launch_both<T, G, 128, XE_SLAB>(both, q, st);
+                else e = one ? launch_both<T, G, 64, XE_OUT>(both, q, st) : launch_both<T, G, 64, XE_SLAB>(both, q, st);
             } else {
                 q.slab = dw_slab; q.ldo = pl.pitch; q.store_n = pl.pitch; q.add = 0;
-                e = launch_mm<T, true, true, XE_SLAB>(q, pl.dw.edge, st);
+                e = launch_mm<T, G, true, true, XE_SLAB>(q, pl.dw.edge, st);
                 if (e == hipSuccess) e = sum_slabs(dw_slab, scale, out, piece, width, pl.pitch, pl.dw.splits, st);
             }
             if (e != hipSuccess) return e;
@@ -1190,11 +1212,13 @@ hipError_t launch_linear_xent(int dtype, int rows, int width, int vocab, const v
 hipError_t launch_linear_xent_bwd(int dtype, int rows, int width, int vocab, const void *x, const void *w, const int64_t *labels, const float *lse,
                                   const float *dloss, void *dx, void *dw, void *ws, hipStream_t st)
 {
-    if (dtype == NGC_BF16)
-        return launch_xent_bwd_t(rows, width, vocab, static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(w), labels, lse, dloss,
-                                 static_cast<uint16_t *>(dx), static_cast<uint16_t *>(dw), static_cast<char *>(ws), st);
-    return launch_xent_bwd_t(rows, width, vocab, static_cast<const float *>(x), static_cast<const float *>(w), labels, lse, dloss,
-                             static_cast<float *>(dx), static_cast<float *>(dw), static_cast<char *>(ws), st);
+    const auto call = [&](auto type, auto g) {
+        typedef decltype(type) T;
+        return launch_xent_bwd_t<T, decltype(g)::value>(rows, width, vocab, static_cast<const T *>(x), static_cast<const T *>(w), labels, lse, dloss,
+                                                        static_cast<T *>(dx), static_cast<T *>(dw), static_cast<char *>(ws), st);
+    };
+    if (dtype == NGC_F32) return call(float(), std::integral_constant<int, 3>());
+    return xent_glimbs(1, rows) == 2 ? call(uint16_t(), std::integral_constant<int, 2>()) : call(uint16_t(), std::integral_constant<int, 1>());
 }
 
 }  // namespace ngc

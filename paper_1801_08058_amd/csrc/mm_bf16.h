@@ -7,9 +7,9 @@
 // global->LDS loads (16 bytes a lane, the scalar base moves along k).  While the products of a stage run, its successor goes from LDS to
 // registers and the stage NS ahead is asked for: one barrier and one counted wait per stage.
 //
-// L = 3: fp32 operands as sums of three bf16 limbs of 8 significant bits each.  Of the nine products of limbs the six that reach 2^-24 of the
-// result are formed.  A stage holds all limbs, so that a 128 x 128 tile has 96 matrix instructions a wave for its 48 KB where a bf16 one has 16
-// for 16 KB.
+// An operand is the sum of PA or PB bf16 limbs of 8 significant bits each.  3, 3: fp32 operands; of the nine products of limbs the six that reach
+// 2^-24 of the result are formed.  2, 1: an fp32 operand that 16 bits hold well enough, with a bf16 one; both products.  A stage holds all limbs, so
+// that a 128 x 128 tile of 3, 3 has 96 matrix instructions a wave for its 48 KB where one of 1, 1 has 16 for 16 KB.
 //
 // LDS of a stage, in units of 16 bytes so that 64 lanes fill 1 KB in lane order:
 //   [R][K] operands   rows of 64 bytes; chunk c of row r sits at c ^ (0 or 3 for r / 8 % 2 = 0 or 1).  ds_read_b128 takes lanes 0-3, 12-15, 20-23
@@ -45,7 +45,7 @@ struct MmParams {
     // there has to be zero, and a [K][.] operand has to hold something behind M or N.
     int M, N, K;
     int mt, nt, splits, kper;    // tiles; parts of the reduction and their length (a multiple of 32)
-    int64_t alimb, blimb;        // L = 3: elements between the limbs of an operand
+    int64_t alimb, blimb;        // elements between the limbs of an operand
 };
 
 constexpr int MM_WAVES = 4;
@@ -126,9 +126,10 @@ struct MmFragments {
     }
 };
 
-// 160 KB of a 256 x 256 tile, two workgroups of a 128 x 128 tile; with three limbs 144 KB of one, two of a 64 x 64 tile
-template <int L> constexpr int mm_stages() { return L == 1 ? 5 : 3; }
-template <int BM, int BN, int L> constexpr int mm_lds_bytes() { return mm_stages<L>() * L * (BM + BN) * 64; }
+// 160 KB of a 256 x 256 tile, two workgroups of a 128 x 128 tile; with three limbs each 144 KB of one, two of a 64 x 64 tile; with two and one two
+// workgroups of a 128 x 128 tile, four of a 64 x 64 tile
+template <int PA> constexpr int mm_stages() { return PA == 1 ? 5 : 3; }
+template <int BM, int BN, int PA, int PB> constexpr int mm_lds_bytes() { return mm_stages<PA>() * (PA * BM + PB * BN) * 64; }
 
 // Two products, c0 += b a0^T and c1 += b a1^T.  Written out so that the accumulators stay where they are: 256 of them fill the accumulation
 // registers, and the compiler moves them about instead of updating them in place.  The leading wait is the one a matrix instruction needs behind
@@ -159,12 +160,12 @@ __device__ __forceinline__ void mm_tile_of(int id, int total, int mt, int nt, in
 }
 
 // acc[fn][fm]: n = 16 fn + 4 (lane / 16) + element, m = 16 fm + lane % 16 of the wave's part
-template <int BM, int BN, bool AT, bool BT, int L>
+template <int BM, int BN, bool AT, bool BT, int PA, int PB>
 __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, int m0, int n0, int k0, int k1, mm_f32x4 (&acc)[BN / 32][BM / 32])
 {
-    constexpr int FM = BM / 32, FN = BN / 32, STAGE = L * (BM + BN) * 64, NS = mm_stages<L>();
-    constexpr int LA = MmOperand<BM, AT>::LOADS * L, LB = MmOperand<BN, BT>::LOADS * L, LPS = LA + LB;
-    static_assert(L == 1 || L == 3, "limbs");
+    constexpr int FM = BM / 32, FN = BN / 32, STAGE = (PA * BM + PB * BN) * 64, NS = mm_stages<PA>();
+    constexpr int LA = MmOperand<BM, AT>::LOADS * PA, LB = MmOperand<BN, BT>::LOADS * PB, LPS = LA + LB;
+    static_assert((PA == 1 && PB == 1) || (PA == 2 && PB == 1) || (PA == 3 && PB == 3), "limbs");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     MmOperand<BM, AT> la;
     MmOperand<BN, BT> lb;
@@ -178,15 +179,15 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
     const unsigned ring = (unsigned)(uintptr_t)(mm_lds_void *)smem;          // LDS address
     auto load = [&](auto whole, int f, unsigned to, int kleft) {             // load f of a stage
         constexpr bool FULL = decltype(whole)::value;
-        if (f < LA) la.template load<FULL>(f % (LA / L), f / (LA / L), p.alimb, to, wave, kleft);
-        else lb.template load<FULL>((f - LA) % (LB / L), (f - LA) / (LB / L), p.blimb, to + L * BM * 64, wave, kleft);
+        if (f < LA) la.template load<FULL>(f % (LA / PA), f / (LA / PA), p.alimb, to, wave, kleft);
+        else lb.template load<FULL>((f - LA) % (LB / PB), (f - LA) / (LB / PB), p.blimb, to + PA * BM * 64, wave, kleft);
     };
     // the PAIRS products of limbs, and the GAPS between pairs of matrix instructions of a stage
-    constexpr int PAIRS = L == 3 ? 6 : 1, GAPS = PAIRS * FN * FM / 2, READS = L * (FM + FN), ITEM_GAPS = GAPS * 3 / 4 > 0 ? GAPS * 3 / 4 : 1;
-    mm_bf16x8 fa[2][L][FM], fb[2][L][FN];
+    constexpr int PAIRS = PA == 3 ? 6 : PA, GAPS = PAIRS * FN * FM / 2, READS = PA * FM + PB * FN, ITEM_GAPS = GAPS * 3 / 4 > 0 ? GAPS * 3 / 4 : 1;
+    mm_bf16x8 fa[2][PA][FM], fb[2][PB][FN];
     auto read = [&](int f, const unsigned char *st, int u) {                 // fragment f of a stage
-        if (f < L * FM) fa[u][f / FM][f % FM] = ra.read(st + f / FM * BM * 64, f % FM);
-        else fb[u][(f - L * FM) / FN][(f - L * FM) % FN] = rb.read(st + L * BM * 64 + (f - L * FM) / FN * BN * 64, (f - L * FM) % FN);
+        if (f < PA * FM) fa[u][f / FM][f % FM] = ra.read(st + f / FM * BM * 64, f % FM);
+        else fb[u][(f - PA * FM) / FN][(f - PA * FM) % FN] = rb.read(st + PA * BM * 64 + (f - PA * FM) / FN * BN * 64, (f - PA * FM) % FN);
     };
 #pragma unroll
     for (int i = 0; i < FN; ++i)
@@ -229,9 +230,9 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
 #pragma unroll
                 for (int f = 0; f < LPS; ++f)
                     if (f * ITEM_GAPS / LPS == q) load(whole, f, to, kleft);
-            // products of limbs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
+            // products of limbs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), or (0,0) (1,0)
             const int pair = q / (FN * FM / 2), i = q % (FN * FM / 2) / (FM / 2), j = q % (FM / 2) * 2;
-            const int l = pair == 5 ? 2 : pair == 2 || pair == 3 ? 1 : 0, r = pair == 4 ? 2 : pair == 1 || pair == 3 ? 1 : 0;
+            const int l = PA == 2 ? pair : pair == 5 ? 2 : pair == 2 || pair == 3 ? 1 : 0, r = PA == 2 ? 0 : pair == 4 ? 2 : pair == 1 || pair == 3 ? 1 : 0;
             mm_pair(acc[i][j], acc[i][j + 1], fb[u][r][i], fa[u][l][j], fa[u][l][j + 1]);
             __builtin_amdgcn_sched_barrier(0);
         }
