@@ -21,9 +21,13 @@ static size_t r256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
-// What the backward pass needs of a row: lse in units of log 2, dloss over the largest |dloss| (0 for rows that do not count), the label (-1)
+// exp(z - top).  The difference comes first: a masked logit may be the lowest number of its type, which times log2 e leaves the range of fp32.  Where all
+// of a part's logits are -inf (or it has none) there is no difference: top 0 makes their exponentials 0.
+__device__ __forceinline__ float exp_below(float z, float top) { return __builtin_amdgcn_exp2f((z - (top == -INFINITY ? 0.f : top)) * LOG2E); }
+
+// What the backward pass needs of a row: lse, dloss over the largest |dloss| (0 for rows that do not count), the label (-1)
 struct XentRow {
-    float lse2, factor;
+    float lse, factor;
     int label, pad;
 };
 
@@ -83,7 +87,7 @@ __global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ la
 #pragma unroll
         for (int b = 0; b < XentRows::B; ++b) {
             const int64_t m = m0 + 1024 * b + threadIdx.x;
-            if (m < rows) info[m] = XentRow{r.l[b] * LOG2E, r.label[b] >= 0 ? r.weight[b] * inv : 0.f, r.label[b] >= 0 ? (int)r.label[b] : -1, 0};
+            if (m < rows) info[m] = XentRow{r.l[b], r.label[b] >= 0 ? r.weight[b] * inv : 0.f, r.label[b] >= 0 ? (int)r.label[b] : -1, 0};
         }
         m0 += (int64_t)gridDim.x * XENT_ROWS;
         if (m0 < rows) r.load(labels, dloss, lse, m0, rows, vocab);
@@ -191,13 +195,12 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top = fmaxf(top, whole || n_ + 16 * i + e < p.mm.N ? acc[i][j][e] : -INFINITY);
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64)) * LOG2E;
-                const float t = top == -INFINITY ? 0.f : top;                    // a wave whose columns are all past the end: sum 0
+                top = fmaxf(top, __shfl_xor(top, 32, 64));                       // -inf: columns past the end (or logits that are -inf) only, sum 0
 #pragma unroll
                 for (int i = 0; i < FN; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float v = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -t));
+                        const float v = exp_below(acc[i][j][e], top);
                         s += whole || n_ + 16 * i + e < p.mm.N ? v : 0.f;
                     }
                 s += __shfl_xor(s, 16, 64);
@@ -218,8 +221,8 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
         for (int r = threadIdx.x; r < BM; r += 64 * MM_WAVES) {
             float2 v = red[r];
             const float2 o = red[BM + r];
-            const float top = fmaxf(v.x, o.x);                                   // the first wave always has columns
-            v = make_float2(top, v.y * __builtin_amdgcn_exp2f(v.x - top) + o.y * __builtin_amdgcn_exp2f(o.x - top));
+            const float top = fmaxf(v.x, o.x);
+            v = make_float2(top, v.y * exp_below(v.x, top) + o.y * exp_below(o.x, top));
             if (tm * BM + r < p.mm.M) p.part[(size_t)tn * p.mm.M + tm * BM + r] = v;
         }
         return;
@@ -249,7 +252,7 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
 #pragma unroll
             for (int i = 0; i < FN; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -row.lse2)) * row.factor;
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = exp_below(acc[i][j][e], row.lse) * row.factor;
             const int label = row.label - p.v0;                                  // few waves hold one
             if (__any(label >= tn * BN + wn && label < tn * BN + wn + BN / 2)) {
 #pragma unroll
@@ -388,15 +391,15 @@ __global__ __launch_bounds__(64 * NW) void xent_row_loss(const float *__restrict
                 up = fmaxf(up, z[b][e]);
                 if (label == v && live) target = z[b][e];
             }
-        s *= __builtin_amdgcn_exp2f((top - up) * LOG2E);                         // 0 the first time
+        s *= exp_below(top, up);                                                 // 0 the first time
         top = up;
 #pragma unroll
         for (int b = 0; b < XENT_BATCH; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((z[b][e] - top) * LOG2E);
+            for (int e = 0; e < 4; ++e) s += exp_below(z[b][e], top);
     }
     const float all = block_reduce<NW>(top, true, sm);
-    s = block_reduce<NW>(top == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f((top - all) * LOG2E), false, sm);
+    s = block_reduce<NW>(s * exp_below(top, all), false, sm);
     if (threadIdx.x) return;
     const float l = all + log2f(s) * LN2;
     lse[m] = l;
@@ -422,7 +425,7 @@ __global__ __launch_bounds__(64 * NW) void xent_row_grad(const float *__restrict
     if (m == 0 && threadIdx.x == 0) *scale = most;
     const int64_t label = m < rows ? labels[m] : -1;
     const bool live = label >= 0 && label < vocab;
-    const float factor = live ? dloss[m] * (1.0f / most) : 0.f, lse2 = live ? lse[m] * LOG2E : 0.f;
+    const float factor = live ? dloss[m] * (1.0f / most) : 0.f, below = live ? lse[m] : 0.f;
     const size_t row = (size_t)(live ? m : 0) * ld;
     for (int w0 = 0; w0 < gp; w0 += 256 * NW * XENT_BATCH) {
         const int v0 = w0 + threadIdx.x * 4;
@@ -439,7 +442,7 @@ __global__ __launch_bounds__(64 * NW) void xent_row_grad(const float *__restrict
             if (v >= gp) break;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                z[b][e] = live && v + e < vocab ? __builtin_amdgcn_exp2f(fmaf(z[b][e], LOG2E, -lse2)) * factor - (label == v + e ? factor : 0.f) : 0.f;
+                z[b][e] = live && v + e < vocab ? exp_below(z[b][e], below) * factor - (label == v + e ? factor : 0.f) : 0.f;
 #pragma unroll
             for (int l = 0; l < G; ++l) {
                 const uint2 q = make_uint2(pack_bf16x2_hw(z[b][0], z[b][1]), pack_bf16x2_hw(z[b][2], z[b][3]));
@@ -774,15 +777,15 @@ __global__ __launch_bounds__(256) void xent_join(const float2 *__restrict__ part
     float top = -INFINITY, s = 0.f;
     if (m < rows)
         for (int t0 = q; t0 < tiles; t0 += 32) {
-            float2 v[4];                                                         // four tiles at a time; the first has a finite maximum
+            float2 v[4];                                                         // four tiles at a time
 #pragma unroll
             for (int b = 0; b < 4; ++b) v[b] = t0 + 8 * b < tiles ? part[(size_t)(t0 + 8 * b) * rows + m] : make_float2(-INFINITY, 0.f);
             float up = top;
 #pragma unroll
             for (int b = 0; b < 4; ++b) up = fmaxf(up, v[b].x);
-            s *= __builtin_amdgcn_exp2f(top - up);
+            s *= exp_below(top, up);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) s += v[b].y * __builtin_amdgcn_exp2f(v[b].x - up);
+            for (int b = 0; b < 4; ++b) s += v[b].y * exp_below(v[b].x, up);
             top = up;
         }
     red[q][r] = make_float2(top, s);
@@ -790,12 +793,11 @@ __global__ __launch_bounds__(256) void xent_join(const float2 *__restrict__ part
     if (q || m >= rows) return;
     for (int i = 1; i < 8; ++i) {
         const float2 v = red[i][r];
-        if (v.x == -INFINITY) continue;                                          // fewer tiles than parts
         const float up = fmaxf(top, v.x);
-        s = s * __builtin_amdgcn_exp2f(top - up) + v.y * __builtin_amdgcn_exp2f(v.x - up);
+        s = s * exp_below(top, up) + v.y * exp_below(v.x, up);
         top = up;
     }
-    const float l = (top + log2f(s)) * LN2;
+    const float l = top + log2f(s) * LN2;
     lse[m] = l;
     loss[m] = labels[m] >= 0 && labels[m] < vocab ? l - target[m] : 0.f;
 }
