@@ -358,8 +358,9 @@ size_t ngc_layer_norm_workspace_bytes(int32_t dtype, int64_t rows, int32_t cols)
 /* Softmax cross entropy of a linear layer: z = x w^T, lse[n] = log sum_v exp z[n][v], loss[n] = lse[n] - z[n][labels[n]].
  * x: [rows, width], w: [vocab, width], both of `dtype`; loss, lse: fp32 [rows].  A row whose label is outside [0, vocab) does not count:
  * its loss is +0 (its lse is written).  The logits are formed tile by tile and not kept (no more than 64 MiB of them at a time, where there are few
- * rows).  Classes may be masked: one whose logit is the lowest number of `dtype`, or below the range of fp32, has probability 0.  A row that counts
- * needs a logit above that.  rows and vocab < 2^28, width < 2^20; rows * width, vocab * width and rows * vocab < 2^37
+ * rows).  Classes may be masked: one whose logit is the lowest number of `dtype`, or below the range of fp32 (no product of two elements past 2^135),
+ * has probability 0.  A row that counts needs a logit above that.  An fp32 element is taken to 2^-24 of itself or to 2^-126, whichever is more.
+ * rows and vocab < 2^28, width < 2^20; rows * width, vocab * width and rows * vocab < 2^37
  * (else NGC_BAD_SHAPE).
  * ws: ngc_linear_xent_workspace_bytes(dtype, rows, width, vocab, 0) bytes. */
 int ngc_linear_xent(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, const void *x, const void *w, const int64_t *labels,

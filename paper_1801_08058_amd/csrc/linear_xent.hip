@@ -95,6 +95,13 @@ __global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ la
     if (blockIdx.x == 0 && threadIdx.x == 0) *scale = top;
 }
 
+// The first limb of a finite value is finite: the numbers above the largest bf16, which would be rounded to infinity, leave up to 2^-8 of themselves to the second
+__device__ __forceinline__ float within_bf16(float v)
+{
+    constexpr float most = 0x1.fep127f;
+    return fminf(fmaxf(v, -most), most);
+}
+
 // Eight values as L limbs: the value rounded to bf16, what that leaves, rounded, and what that leaves (one limb: values that bf16 holds)
 template <int L>
 __device__ __forceinline__ void split_limbs(const float (&f)[8], mm_bf16x8 (&out)[L])
@@ -107,7 +114,7 @@ __device__ __forceinline__ void split_limbs(const float (&f)[8], mm_bf16x8 (&out
         uint32_t w[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            w[k] = pack_bf16x2_hw(r[2 * k], r[2 * k + 1]);
+            w[k] = L > 1 && q == 0 ? pack_bf16x2_hw(within_bf16(r[2 * k]), within_bf16(r[2 * k + 1])) : pack_bf16x2_hw(r[2 * k], r[2 * k + 1]);
             r[2 * k] -= __uint_as_float(w[k] << 16);
             r[2 * k + 1] -= __uint_as_float(w[k] & 0xFFFF0000u);
         }
@@ -814,7 +821,7 @@ __global__ __launch_bounds__(256) void xent_pad(const T *__restrict__ src, uint1
             float b = r < rows && j + 1 < width ? SmElem<T>::load(src + (size_t)r * width + j + 1) : 0.f;
 #pragma unroll
             for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
-                const uint32_t q = pack_bf16x2_hw(a, b);
+                const uint32_t q = sizeof(T) == 4 && l == 0 ? pack_bf16x2_hw(within_bf16(a), within_bf16(b)) : pack_bf16x2_hw(a, b);
                 *reinterpret_cast<uint32_t *>(dst + l * limb + (size_t)r * pitch + j) = q;
                 a -= __uint_as_float(q << 16);
                 b -= __uint_as_float(q & 0xFFFF0000u);

@@ -230,8 +230,9 @@ __device__ __forceinline__ void mm_tile(const MmParams &p, unsigned char *smem, 
 #pragma unroll
                 for (int f = 0; f < LPS; ++f)
                     if (f * ITEM_GAPS / LPS == q) load(whole, f, to, kleft);
-            // products of limbs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), or (0,0) (1,0)
-            const int pair = q / (FN * FM / 2), i = q % (FN * FM / 2) / (FM / 2), j = q % (FM / 2) * 2;
+            // products of limbs (2,0) (0,2) (1,1) (1,0) (0,1) (0,0), or (1,0) (0,0): the largest last, so that the first two limbs of the largest numbers,
+            // which may be 2^128 together, meet behind the third
+            const int pair = PAIRS - 1 - q / (FN * FM / 2), i = q % (FN * FM / 2) / (FM / 2), j = q % (FM / 2) * 2;
             const int l = PA == 2 ? pair : pair == 5 ? 2 : pair == 2 || pair == 3 ? 1 : 0, r = PA == 2 ? 0 : pair == 4 ? 2 : pair == 1 || pair == 3 ? 1 : 0;
             mm_pair(acc[i][j], acc[i][j + 1], fb[u][r][i], fa[u][l][j], fa[u][l][j + 1]);
             __builtin_amdgcn_sched_barrier(0);

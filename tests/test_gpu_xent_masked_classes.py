@@ -40,7 +40,7 @@ def _masked(kind, vocab):
 
 
 # the logits in parts, in tiles of each size (rows above what the parts take, many rows), straight from memory (fp32, odd bf16 widths over many classes)
-CASES = [("bf16", 5, 64, 900), ("bf16", 130, 72, 5003), ("bf16", 1100, 40, 3001), ("bf16", 3, 67, 9001),
+CASES = [("bf16", 5, 64, 900), ("bf16", 130, 72, 5003), ("bf16", 1100, 40, 3001), ("bf16", 3, 67, 9001), ("f32", 5, 64, 900), ("f32", 40, 33, 9001), ("f32", 1100, 40, 3001),
          ("bf16", 9000, 16, 300)]
 
 
