@@ -82,8 +82,9 @@ struct MmOperand {
         }
     }
     // Load i of limb l (`limb` elements from limb to limb) of the stage.  kleft: k that are left from this stage on; FULL: at least 32.  The load
-    // goes straight to LDS and has no result register.  It is written out because the compiler waits for every such load that it knows of in front of a transposing LDS read, whatever
-    // part of the ring that reads; the waits that are needed are those of mm_tile.
+    // goes straight to LDS and has no result register.  It is written out because the compiler waits for every such load that it knows of in front of
+    // a transposing LDS read, whatever part of the ring that reads.  It is not said to write memory: LDS reads may move across it, as what they read
+    // is not what it writes.  The order of a place in the ring is that of mm_tile's counted waits and barriers, which nothing moves across.
     template <bool FULL>
     __device__ __forceinline__ void load(int i, int l, int64_t limb, unsigned lds, int wave, int kleft) const
     {
@@ -91,7 +92,8 @@ struct MmOperand {
         const uint64_t at = base + 2 * l * limb;
         const u32x4 rs = {(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, 0x7fffffffu, 0x00020000u};
         const unsigned v = FULL || kin(i, wave) < kleft ? voff[i] : MM_OOB;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + (unsigned)((l * LOADS + i) * NW + wave) * 1024u), "v"(v), "s"(rs));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + (unsigned)((l * LOADS + i) * NW + wave) * 1024u), "v"(v), "s"(rs)
+                     : "m0");
     }
     __device__ __forceinline__ void next() { base += step; }
 };
