@@ -917,6 +917,8 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
     if (bwd && piece > most / p.glimbs / p.krows) piece = most / p.glimbs / p.krows;
     if (piece > most / p.limbs / p.pitch) piece = most / p.limbs / p.pitch;
     if (piece > (1 << 21)) piece = 1 << 21;                              // offsets in a tile of g stay below 2 GiB
+    const char *cap = env_switch(SW_XENT_PIECE);
+    if (cap && piece > atoi(cap)) piece = atoi(cap);
     p.piece = (int)(piece >= vocab ? vocab : piece < 256 ? 256 : piece / 256 * 256);
     if (p.piece > vocab) p.piece = vocab;
     // only copies and gradients make pieces of the vocabulary (copies are also made of tensors off the 16-byte grid)
@@ -932,7 +934,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         p.by_rows = parts.us < p.z.us && (int64_t)rows * up(vocab, 8) * 4 * parts.splits <= (32 << 20);
         if (p.by_rows) p.z = parts;
     }
-    if (p.copy && rows <= few_rows(p.limbs) && vocab >= XENT_FEW_VOCAB && (int64_t)rows * up(vocab, 8) * 4 <= (64 << 20) && vocab <= (1 << 21)) {
+    if (p.copy && rows <= few_rows(p.limbs) && vocab >= XENT_FEW_VOCAB && !(cap && p.piece < vocab) && (int64_t)rows * up(vocab, 8) * 4 <= (64 << 20) && vocab <= (1 << 21)) {
         p.few = p.by_rows = true;
         p.few_dw = rows <= (p.limbs == 3 ? 32 : 16);
         p.piece = vocab;

@@ -128,7 +128,7 @@ def test_special_rows(dtype, kind):
     _check(dtype, x, w, labels, dloss)
 
 
-# a vocabulary of several pieces, rows and products split over many workgroups
+# rows and products split over many workgroups
 @pytest.mark.parametrize("dtype,rows,width,vocab", [("bf16", 1030, 64, 5003), ("bf16", 2, 2048, 32000), ("f32", 3, 512, 20011), ("bf16", 4200, 24, 333),
                                                     ("f32", 700, 100, 3000), ("bf16", 600, 640, 9000)])
 def test_long_axes(dtype, rows, width, vocab):
