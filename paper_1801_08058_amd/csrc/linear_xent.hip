@@ -870,13 +870,18 @@ static MmChoice mm_choose(int64_t m, int64_t n, int64_t k, int pa, int pb, int m
     // what memory takes for the operands: a small tile is no faster than a large one then
     const float bytes = ((float)m * (float)pa + (float)n * (float)pb) * (float)k * 2.f / 4.4e6f;
     MmChoice best = {64, 1, INFINITY};
+    // a forced tile that slabs do not have is no choice of theirs; one that no form of these operands has is left alone
+    const int largest = pa > 1 || slab ? 128 : 256;
     const char *forced = env_switch(SW_XENT_TILE);
-    for (int edge = pa > 1 || slab ? 128 : 256; edge >= 64; edge /= 2)
+    int only = forced ? atoi(forced) : 0;
+    if (only > largest && slab) return best;
+    if (only > largest) only = 0;
+    for (int edge = largest; edge >= 64; edge /= 2)
         for (int p : parts) {
             if (p > most || (p > 1 && k / p < 128)) break;
             if (edge < 128 && ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * p > (1 << 22)) break;      // a grid holds fewer than 2^32 threads
             const float run = mm_expected(edge, pa, m, n, stages, p), t = (run > bytes ? run : bytes) + (p > 1 || slab ? 3.f + (float)m * (float)n * 8.f * (float)p / 4e6f : 0.f);
-            if (t < best.us && (!forced || atoi(forced) == edge || (slab && best.us == INFINITY))) best = {edge, p, t};
+            if (t < best.us && (!only || only == edge)) best = {edge, p, t};
         }
     return best;
 }

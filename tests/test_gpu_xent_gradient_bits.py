@@ -26,12 +26,7 @@ def _gradients(x, w, labels, lse, dloss, offset):
     return dx.f64(rows, width), dw.f64(vocab, width)
 
 
-# the logits in parts, in tiles (one row over 70001 classes of 256; 128 rows over 9000), straight from memory (odd widths over many classes)
-@pytest.mark.parametrize("offset", [0, 1])
-@pytest.mark.parametrize("rows,width,vocab", [(1, 8, 2), (1, 64, 300), (2, 515, 777), (17, 130, 1000), (128, 256, 1000), (1, 256, 70001), (100, 72, 9000), (128, 512, 9000),
-                                              (1, 33, 8192), (16, 67, 8221), (17, 131, 8195), (32, 515, 10007), (33, 129, 8300), (128, 8, 33)])
-def test_few_rows_keep_sixteen_bits_of_g(rows, width, vocab, offset):
-    print(f"linear_xent bits {rows} {width} {vocab} offset {offset}", flush=True)
+def _check(rows, width, vocab, offset):
     x, w, labels, dloss = _inputs("bf16", rows, width, vocab, 7 * rows + width + vocab, dead=0.1 if rows > 4 else 0.0)
     x64, w64 = x.astype(np.float64), w.astype(np.float64)
     lse = oracle.linear_xent(x, w, labels)[1].astype(np.float32)
@@ -49,3 +44,20 @@ def test_few_rows_keep_sixteen_bits_of_g(rows, width, vocab, offset):
         tol = dd @ other + (k + 8) * U * (gg @ other) + 2.0 ** -8 * np.abs(ref) + 2.0 ** -126
         err = np.abs(got - ref)
         assert (err <= tol * 1.01).all(), (err - tol).max()
+
+
+# the logits in parts, in tiles (one row over 70001 classes of 256; 128 rows over 9000), straight from memory (odd widths over many classes)
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("rows,width,vocab", [(1, 8, 2), (1, 64, 300), (2, 515, 777), (17, 130, 1000), (128, 256, 1000), (1, 256, 70001), (100, 72, 9000), (128, 512, 9000),
+                                              (1, 33, 8192), (16, 67, 8221), (17, 131, 8195), (32, 515, 10007), (33, 129, 8300), (128, 8, 33)])
+def test_few_rows_keep_sixteen_bits_of_g(rows, width, vocab, offset):
+    print(f"linear_xent bits {rows} {width} {vocab} offset {offset}", flush=True)
+    _check(rows, width, vocab, offset)
+
+
+@pytest.mark.parametrize("edge", [64, 128, 256])
+@pytest.mark.parametrize("rows,width,vocab", [(1, 16, 70), (3, 515, 1003), (100, 72, 777), (128, 264, 2500), (65, 130, 129)])
+def test_sixteen_bits_with_every_tile(monkeypatch, rows, width, vocab, edge):
+    print(f"linear_xent bits edge {edge} {rows} {width} {vocab}", flush=True)
+    monkeypatch.setenv("NGC_XENT_TILE", str(edge))
+    _check(rows, width, vocab, 0)
