@@ -61,3 +61,44 @@ def test_sixteen_bits_with_every_tile(monkeypatch, rows, width, vocab, edge):
     print(f"linear_xent bits edge {edge} {rows} {width} {vocab}", flush=True)
     monkeypatch.setenv("NGC_XENT_TILE", str(edge))
     _check(rows, width, vocab, 0)
+
+
+# parts, tiles, weights straight from memory
+@pytest.mark.parametrize("rows,width,vocab", [(128, 256, 1000), (17, 512, 9000), (5, 67, 9001)])
+def test_captured_calls_replay_bit_for_bit(rows, width, vocab):
+    print(f"linear_xent bits graph {rows} {width} {vocab}", flush=True)
+    need = max(ng.ngc_linear_xent_workspace_bytes(ng.NGC_BF16, rows, width, vocab, b) for b in (0, 1))
+    new = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t, device="cuda")
+    x, w, dx, dw, labels, ws = new(rows, width), new(vocab, width), new(rows, width), new(vocab, width), new(rows, t=torch.int64), new(need, t=torch.uint8)
+    loss, lse, dloss = (new(rows, t=torch.float32) for _ in range(3))
+    outs = (loss, lse, dx, dw)
+
+    def run(st):
+        ng.ngc_linear_xent(ng.NGC_BF16, rows, width, vocab, x, w, labels, loss, lse, ws, st)
+        ng.ngc_linear_xent_bwd(ng.NGC_BF16, rows, width, vocab, x, w, labels, lse, dloss, dx, dw, ws, st)
+
+    def load(seed):
+        for t, a in zip((x, w, labels, dloss), _inputs("bf16", rows, width, vocab, seed)):
+            t.copy_(torch.from_numpy(np.ascontiguousarray(a)))
+
+    load(1)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        run(side.cuda_stream)                            # eager: one-time kernel attributes are set outside the capture
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            run(torch.cuda.current_stream().cuda_stream)
+    for seed in (2, 3, 4):
+        load(seed)
+        run(stream())
+        torch.cuda.synchronize()
+        eager = [t.clone() for t in outs]
+        for t in outs:
+            t.fill_(float("nan"))
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager)), seed
