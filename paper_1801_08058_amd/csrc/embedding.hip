@@ -77,8 +77,8 @@ hipError_t launch_embedding(int dtype, int64_t tokens, int vocab, int width, flo
 // Up to 8192 tokens take three launches: each range looks through all tokens itself (from the L2), which costs less than a launch that sorts
 // blocks (5001 tokens, 10007 rows of 777, fp32, all launches: 31.8 -> 27 us; 18935 tokens: 7.6 us for launch 1 alone).  Above,
 // the looking grows with tokens x ranges.
-// Bound: HBM, dy read once and dtable written once (16384 tokens of 2048 bf16 over 32000 rows: 88 us for 329 MB; launches 10, 44 with the zeros of
-// 25000 rows, 6 and 27 us).
+// Bound: HBM, dy read once and dtable written once (16384 tokens of 2048 bf16 over 32000 rows: 88 us for 329 MB; launches, timed each by itself, 11, 48 with the
+// zeros of 25000 rows, 6 and 30 us).
 constexpr int EMB_RANGES = 2048, EMB_BLOCKS = 512, EMB_TILE = 2048, EMB_SCAN = 8192;
 // Waves of a range's workgroup: the range of the frequent ids may hold a third of the tokens (18935 tokens, 18913 rows of 64: launch 2 takes 26 us
 // with four, 17 with eight)

@@ -12,7 +12,8 @@
 // same lanes add up their columns' dgamma and dbeta over the group's rows; the groups' sums are joined by a second launch in a fixed order.
 // Rows that are no multiple of 16 bytes end in a vector that overlaps the one before it, as softmax's.  Rows beyond the registers take a
 // workgroup each and three passes (backprop two, and the columns' sums a pass of their own); rows below 16 bytes a thread each.
-// 16384 x 4096 bf16: forward 43 us, 6.2 TB/s; backprop 75 us, 5.4 TB/s, and 5 us for the second launch.  8 rows: 3.4 us.
+// 16384 x 4096 bf16: forward 43 us, 6.2 TB/s; backprop 76 us, 5.3 TB/s, and 5 us for the second launch.  8 rows: 3.5 us.  Backprop of 4096 fp32 rows: 8192
+// columns, in registers, 78 + 5 us, 5.2 TB/s; 16384, beyond them, 191 + 98 + 5 us, as x and dy are read three times.
 #include "rows.h"
 
 namespace ngc {

@@ -7,9 +7,9 @@
 // for a piece of the vocabulary at a time.  All products run on the bf16 matrix cores (mm_bf16.h); fp32 tensors as three limbs of bf16, which
 // six products of limbs multiply as exactly as fp32 arithmetic does, at a sixth of the bf16 rate: the fp32 matrix instructions have a sixteenth.
 //
-// Bound: matrix pipes; few rows HBM, the weight read once per product (1 x 4096 over 50257 classes bf16: 90 us, 4.5 TB/s); few rows and classes
-// the chain of launches (128 x 2048 over 1000 classes: five of 4 to 9 us).  8192 x 4096 over 50257 classes bf16: loss 2.7 ms, with gradients 10.5 ms
-// of which the logits, formed again, are 2.8.
+// Bound: matrix pipes; few rows HBM, the weight read once per product (loss of 1 x 4096 over 50257 classes bf16: 99 us, 4.2 TB/s); few rows and classes
+// the chain of launches (128 x 2048 over 1000 classes: six of 4 to 9 us).  8192 x 4096 over 50257 classes bf16: loss 2.8 ms, with gradients 10.7 ms
+// of which the logits, formed again, are 2.9.
 #include "mm_bf16.h"
 #include "rows.h"
 
@@ -463,8 +463,8 @@ __global__ __launch_bounds__(64 * NW) void xent_row_grad(const float *__restrict
 // ---- few rows, and a weight that the products above would have to copy (fp32, rows of no multiple of 16 bytes) ----
 //
 // The weight goes straight from memory to registers, at any alignment, and becomes limbs there: it is read once per product, where a copy
-// reads it, writes three bf16 values per element and reads those.  Bound: HBM (fp32, 33024 classes of 1024: 27 us for 8 rows, 5.0 TB/s, 47 for 64);
-// bf16 rows of odd lengths the L1, which serves loads off the 4-byte grid in pieces (54005 classes of 2541, 18 rows: 108 us, fp32 143).
+// reads it, writes three bf16 values per element and reads those.  Bound: HBM (fp32, 33024 classes of 1024: 29 us for 8 rows, 4.7 TB/s, 48 for 64);
+// bf16 rows of odd lengths the L1, which serves loads off the 4-byte grid in pieces (54005 classes of 2541, 18 rows: 109 us, fp32 150).
 
 // The k of element e of lane group g within a step of 32: a lane's 16 bytes, and with them 64 bytes of a row in one load, lie together
 template <typename T> __host__ __device__ constexpr int few_k(int g, int e) { return sizeof(T) == 4 ? 16 * (e / 4) + 4 * g + e % 4 : 8 * g + e; }
@@ -621,7 +621,8 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
     for (int j = 0; j < MT; ++j) xr[j] = gr + (size_t)(m0 + 16 * j + l < rows ? m0 + 16 * j + l : rows - 1) * gp;
     // A step is 32 classes, of which a lane holds four columns of eight.  A lane whose four columns end behind the row loads the row's last four, of
     // which the products take what is theirs (shift).  fp32: one step ahead (a ring of two, unrolled, takes 216 registers instead of 160: 187 against
-    // 131 us for 54005 classes of 2541); bf16 steps are half as long, three ahead and g with them (146 -> 80 us).
+    // 131 us for 54005 classes of 2541); bf16 steps are half as long, three ahead and g with them (146 -> 80 us with one
+    // limb of g, 84 with both).
     struct Step {
         uint32_t w[8][sizeof(T)];                                                // four elements
         uint4 g[L == 1 ? MT : 1][G];
@@ -724,7 +725,7 @@ __global__ __launch_bounds__(256) void xent_few_dx(const uint16_t *__restrict__ 
 
 // dw[v][d] = scale sum_m g[m][v] x[m][d] of at most R rows: a thread keeps four columns of x and stores them for class after class.  A workgroup
 // takes 64 classes, their g in LDS, and 4 LPR columns; 256 / LPR classes at a time.  Bound: HBM for 16 rows, with 32 the vector instructions (fp32,
-// 54005 x 2541: 187 us, the matrix cores' tile 208; bf16 184 and 114, so 16 at most).
+// 54005 x 2541: 190 us, the matrix cores' tile 208; bf16 184 and 121, so 16 at most).
 template <typename T, int R, int LPR>
 __global__ __launch_bounds__(256) void xent_few_dw(const uint16_t *__restrict__ gr, int64_t glimb, int gp, const T *__restrict__ x, const float *__restrict__ scale,
                                                    T *__restrict__ dw, int rows, int width, int vocab)
@@ -901,7 +902,7 @@ struct XentPlan {
 static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
 
 // Rows that the kernels for few rows take, 16, 32 or (fp32) 64 a workgroup; fp32 in two groups, which read the weight again.  Loss and gradients over
-// 33171 classes of 1921, with copies and without: bf16 292 -> 226 us for 1 row, 308 -> 299 for 30, 317 -> 325 for 40; fp32 716 -> 328 for 30,
+// 33171 classes of 1921, with copies and without: bf16 321 -> 218 us for 1 row, 345 -> 296 for 30 (40: 317 -> 325 with one limb of g); fp32 716 -> 328 for 30,
 // 796 -> 432 for 60, and 495 -> 384 for 100 rows over 33000 of 1000.  Fewer than 8192 classes are fewer than 256 waves, and their copy is short
 // (128 x 2048 over 1000 classes fp32: 121 us without, 25 with copies).
 constexpr int XENT_FEW_VOCAB = 8192;

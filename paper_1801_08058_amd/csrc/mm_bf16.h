@@ -19,9 +19,9 @@
 //                     ds_read_b64_tr_b16 turns 4 k x 16 columns into four k of one column per lane: two lane groups touch every bank once
 // Rows and k past the ends are read as zeros: lanes whose offset is past the range of the buffer descriptor.
 //
-// Bound: matrix pipes, at the clock that the power allows (about 2 GHz under this load).  8192 x 4096 x 50257 bf16, 256 x 256 tiles: 1.26 PFLOP/s as
-// x w^T, 1.34 as g w, 1.24 as g^T x, the pipes busy 0.62 to 0.69 of the cycles, no LDS bank conflicts (an 8192^3 library product: 1.38 and 1.20).
-// Three limbs, 128 x 128 tiles: 1.1 us a stage, 198 TFLOP/s of fp32 (library: 150).
+// Bound: matrix pipes, at the clock that the power allows (about 2 GHz under this load).  8192 x 4096 x 50257 bf16, 256 x 256 tiles: 1.21 PFLOP/s as
+// x w^T (1.17 with the epilogue of g), 1.31 as g w, 1.21 as g^T x, the pipes busy 0.60 to 0.68 of the cycles, no LDS bank conflicts (an 8192^3 library
+// product: 1.38 and 1.20).  Three limbs, 128 x 128 tiles: 1.1 us a stage, 4096 x 4096 x 32768 at 205 TFLOP/s of fp32 (library: 150).
 #pragma once
 #include "common.h"
 
