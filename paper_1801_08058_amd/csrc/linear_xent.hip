@@ -190,8 +190,8 @@ __device__ __forceinline__ void xent_product(const XentMm &p, int block)
         int label[FM];                                                           // class of the piece, or -1
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
-            const int64_t at = m_ + 16 * j < p.mm.M ? p.labels[m_ + 16 * j] - p.v0 : -1;
-            label[j] = at >= 0 && at < p.mm.N ? (int)at : -1;
+            const uint64_t at = m_ + 16 * j < p.mm.M ? (uint64_t)p.labels[m_ + 16 * j] - (uint64_t)p.v0 : ~0ull;     // in front of the piece: huge
+            label[j] = at < (uint64_t)p.mm.N ? (int)at : -1;
         }
         auto rows = [&](auto whole) {                                            // whole: no columns past the end, which count nothing
 #pragma unroll
@@ -501,7 +501,7 @@ struct Eight {
     }
 };
 
-template <typename T> constexpr int few_g() { return sizeof(T) == 4 ? 3 : 2; }          // limbs of g: bf16 has fewer than XENT_FINE_ROWS rows here
+template <typename T> constexpr int few_g() { return sizeof(T) == 4 ? 3 : 2; }          // limbs of g
 
 // blocks of 16 classes of a workgroup: more rows of x, which every workgroup reads, more classes for them
 constexpr int xent_few_blocks(int mt) { return mt == 1 ? 2 : 4; }
@@ -907,6 +907,7 @@ static int64_t up(int64_t v, int to) { return (v + to - 1) / to * to; }
 // (128 x 2048 over 1000 classes fp32: 121 us without, 25 with copies).
 constexpr int XENT_FEW_VOCAB = 8192;
 static int few_rows(int limbs) { return limbs == 3 ? 128 : 32; }
+static_assert(XENT_FINE_ROWS >= 32, "the kernels for few rows take two limbs of g");
 static int few_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }       // blocks of 16 rows of a workgroup
 static int few_groups(int64_t rows) { return (int)((rows + 63) / 64); }                  // workgroups for all rows
 
