@@ -99,7 +99,7 @@ __global__ __launch_bounds__(1024) void xent_rows(const int64_t *__restrict__ la
 __device__ __forceinline__ float within_bf16(float v)
 {
     constexpr float most = 0x1.fep127f;
-    return fminf(fmaxf(v, -most), most);
+    return __builtin_amdgcn_fmed3f(v, -most, most);
 }
 
 // Eight values as L limbs: the value rounded to bf16, what that leaves, rounded, and what that leaves (one limb: values that bf16 holds)
