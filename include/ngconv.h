@@ -368,8 +368,8 @@ int ngc_linear_xent(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, c
 
 /* Its gradients: g[n][v] = (exp(z[n][v] - lse[n]) - [v = labels[n]]) * dloss[n], 0 for the rows that do not count; dx = g w, dw = g^T x, both
  * of `dtype`, overwritten; either (not both) may be NULL.  lse: of the forward call on the same x and w; dloss: fp32 [rows] (1 / count for a
- * mean); neither is used in rows that do not count.  For bf16 operands the products take g with 16 bits (2^-16 of its value) up to 128 rows, rounded to bf16
- * (2^-8 of its value at most) for more.  The logits are formed again, a piece of the vocabulary at a time.
+ * mean); neither is used in rows that do not count.  For bf16 operands the products take g with 16 bits (2^-16 of its value) up to 128 rows or
+ * rows * width * vocab = 2^31, rounded to bf16 (2^-8 of its value at most) in larger calls.  The logits are formed again, a piece of the vocabulary at a time.
  * ws: ngc_linear_xent_workspace_bytes(dtype, rows, width, vocab, 1) bytes. */
 int ngc_linear_xent_bwd(int32_t dtype, int64_t rows, int32_t width, int32_t vocab, const void *x, const void *w, const int64_t *labels,
                         const float *lse, const float *dloss, void *dx, void *dw, void *ws, size_t ws_bytes, void *hip_stream);

@@ -137,14 +137,21 @@ __device__ __forceinline__ mm_f32x4 limb_products(const mm_bf16x8 (&a)[PA], cons
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[0], c, 0, 0, 0);
 }
 
-// g as an operand of dx and dw has the three limbs of fp32 tensors, and of bf16 tensors two (16 bits) up to this many rows, one (rounded to bf16) of
-// more.  The rounding of the g at a label is the same in all elements of the row's dx that come from it, and in those of the label's dw: with one
-// limb the distance from exact gradients is 0.0018 to 0.0022 of their norm, with two the 0.0017 that rounding the results leaves (1 to 2048 rows).  Two limbs are
-// twice the matrix instructions.  Up to about this many rows memory and the launches bound dx and dw; above them those instructions do.  Loss and
-// gradients with one limb and with two, 2048 wide over 32000 classes: 111 -> 117 us for 8 rows, 152 -> 175 for 128, 207 -> 254 for 256, 0.95 -> 1.47
-// ms for 2048; 8192 x 4096 over 50257: 10.7 -> 18.3 ms.
+// g as an operand of dx and dw has the three limbs of fp32 tensors, and of bf16 tensors two (16 bits) up to XENT_FINE_ROWS rows or XENT_FINE_WORK multiply-adds
+// of a product, one (rounded to bf16) in larger calls.  The rounding of the g at a label is the same in all elements of the row's dx that come from it, and
+// in those of the label's dw: with one limb the distance from exact gradients is 0.0018 to 0.0022 of their norm, with two the 0.0017 that rounding the
+// results leaves (1 to 2048 rows).  Two limbs are twice the matrix instructions.  In small calls and with few rows launches and memory bound dx and dw, above
+// that those instructions do.  Loss and gradients with one limb and with two: 128 x 2048 over 1000 classes 28 -> 30 us, 1000 x 512 over 1000 29 -> 32,
+// 1024 x 1024 over 2048 46 -> 53; 2048 wide over 32000 classes 111 -> 117 us for 8 rows, 152 -> 175 for 128, 207 -> 254 for 256, 0.95 -> 1.47 ms for 2048; 2048 x
+// 2048 over 2048 91 -> 143 us; 8192 x 4096 over 50257 10.7 -> 18.3 ms.
 constexpr int XENT_FINE_ROWS = 128;
-static int xent_glimbs(int limbs, int64_t rows) { return limbs == 3 ? 3 : rows <= XENT_FINE_ROWS ? 2 : 1; }
+constexpr double XENT_FINE_WORK = 2147483648.0;
+static int xent_glimbs(int limbs, int64_t rows, int width, int vocab)
+{
+    const char *forced = env_switch(SW_XENT_LIMBS);
+    if (forced && limbs == 1) return atoi(forced) == 2 ? 2 : 1;
+    return limbs == 3 ? 3 : rows <= XENT_FINE_ROWS || (double)rows * (double)width * (double)vocab <= XENT_FINE_WORK ? 2 : 1;
+}
 
 // T: uint16_t (bf16) or float (in limbs)
 enum XentEpilogue { XE_STATS, XE_GRAD, XE_SLAB, XE_OUT };
@@ -915,7 +922,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
 {
     XentPlan p{};
     p.limbs = dtype == NGC_F32 ? 3 : 1;
-    p.glimbs = xent_glimbs(p.limbs, rows);
+    p.glimbs = xent_glimbs(p.limbs, rows, width, vocab);
     p.pitch = (int)up(width, p.limbs == 3 ? 32 : 8);
     p.copy = p.limbs == 3 || p.pitch != width;
     p.krows = p.limbs == 3 ? up(rows, 32) : rows;
@@ -941,7 +948,7 @@ static XentPlan xent_plan(int dtype, int64_t rows, int width, int vocab, bool bw
         p.by_rows = parts.us < p.z.us && (int64_t)rows * up(vocab, 8) * 4 * parts.splits <= (32 << 20);
         if (p.by_rows) p.z = parts;
     }
-    if (p.copy && rows <= few_rows(p.limbs) && vocab >= XENT_FEW_VOCAB && !(cap && p.piece < vocab) && (int64_t)rows * up(vocab, 8) * 4 <= (64 << 20) && vocab <= (1 << 21)) {
+    if (p.copy && rows <= few_rows(p.limbs) && vocab >= XENT_FEW_VOCAB && p.glimbs > 1 && !(cap && p.piece < vocab) && (int64_t)rows * up(vocab, 8) * 4 <= (64 << 20) && vocab <= (1 << 21)) {
         p.few = p.by_rows = true;
         p.few_dw = rows <= (p.limbs == 3 ? 32 : 16);
         p.piece = vocab;
@@ -1236,7 +1243,7 @@ hipError_t launch_linear_xent_bwd(int dtype, int rows, int width, int vocab, con
                                                         static_cast<T *>(dx), static_cast<T *>(dw), static_cast<char *>(ws), st);
     };
     if (dtype == NGC_F32) return call(float(), std::integral_constant<int, 3>());
-    return xent_glimbs(1, rows) == 2 ? call(uint16_t(), std::integral_constant<int, 2>()) : call(uint16_t(), std::integral_constant<int, 1>());
+    return xent_glimbs(1, rows, width, vocab) == 2 ? call(uint16_t(), std::integral_constant<int, 2>()) : call(uint16_t(), std::integral_constant<int, 1>());
 }
 
 }  // namespace ngc

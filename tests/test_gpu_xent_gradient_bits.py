@@ -1,5 +1,5 @@
-"""The gradients of ngc_linear_xent_bwd for few rows of bf16: g enters its products with 16 bits, so that dx and dw are one rounding away from
-those of an exact g.  Elementwise bounds as in test_gpu_linear_xent.py, with g's rounding at two half steps of bf16 on top of each other,
+"""The gradients of ngc_linear_xent_bwd for few rows of bf16, and for more where the products are small: g enters its products with 16 bits, so that
+dx and dw are one rounding away from those of an exact g.  Elementwise bounds as in test_gpu_linear_xent.py, with g's rounding at two half steps of bf16 on top of each other,
 2^-8 of its value times 2^-8, in the place of one."""
 import numpy as np
 import pytest
@@ -49,6 +49,7 @@ def _check(rows, width, vocab, offset):
 # the logits in parts, in tiles (one row over 70001 classes of 256; 128 rows over 9000), straight from memory (odd widths over many classes)
 @pytest.mark.parametrize("offset", [0, 1])
 @pytest.mark.parametrize("rows,width,vocab", [(1, 8, 2), (1, 64, 300), (2, 515, 777), (17, 130, 1000), (128, 256, 1000), (1, 256, 70001), (100, 72, 9000), (128, 512, 9000),
+                                              (300, 515, 777), (1000, 128, 500), (1030, 64, 5003), (8193, 24, 40), (5000, 33, 300), (129, 520, 2049), (1024, 1024, 2048),
                                               (1, 33, 8192), (16, 67, 8221), (17, 131, 8195), (32, 515, 10007), (33, 129, 8300), (128, 8, 33)])
 def test_few_rows_keep_sixteen_bits_of_g(rows, width, vocab, offset):
     print(f"linear_xent bits {rows} {width} {vocab} offset {offset}", flush=True)
@@ -56,7 +57,7 @@ def test_few_rows_keep_sixteen_bits_of_g(rows, width, vocab, offset):
 
 
 @pytest.mark.parametrize("edge", [64, 128, 256])
-@pytest.mark.parametrize("rows,width,vocab", [(1, 16, 70), (3, 515, 1003), (100, 72, 777), (128, 264, 2500), (65, 130, 129)])
+@pytest.mark.parametrize("rows,width,vocab", [(1, 16, 70), (3, 515, 1003), (100, 72, 777), (128, 264, 2500), (65, 130, 129), (700, 72, 1003)])
 def test_sixteen_bits_with_every_tile(monkeypatch, rows, width, vocab, edge):
     print(f"linear_xent bits edge {edge} {rows} {width} {vocab}", flush=True)
     monkeypatch.setenv("NGC_XENT_TILE", str(edge))
@@ -64,7 +65,7 @@ def test_sixteen_bits_with_every_tile(monkeypatch, rows, width, vocab, edge):
 
 
 # parts, tiles, weights straight from memory
-@pytest.mark.parametrize("rows,width,vocab", [(128, 256, 1000), (17, 512, 9000), (5, 67, 9001)])
+@pytest.mark.parametrize("rows,width,vocab", [(128, 256, 1000), (17, 512, 9000), (5, 67, 9001), (2000, 64, 3000)])
 def test_captured_calls_replay_bit_for_bit(rows, width, vocab):
     print(f"linear_xent bits graph {rows} {width} {vocab}", flush=True)
     need = max(ng.ngc_linear_xent_workspace_bytes(ng.NGC_BF16, rows, width, vocab, b) for b in (0, 1))
